@@ -50,10 +50,15 @@ namespace {
 
 thread_local char g_hip_msg[256] = "no HIP error recorded";
 
-int hip_fail(hipError_t e, const char* what) {
+}  // namespace
+
+int csd::hip_fail(hipError_t e, const char* what) {
   snprintf(g_hip_msg, sizeof g_hip_msg, "HIP error in %s: %s", what, hipGetErrorString(e));
   return CSD_ERR_HIP;
 }
+
+namespace {
+
 #define CSD_HIP(call)                                   \
   do {                                                  \
     hipError_t e_ = (call);                             \

@@ -7,6 +7,9 @@
 
 namespace csd {
 
+// keeps the text that csd_strerror gives for CSD_ERR_HIP, which it returns
+int hip_fail(hipError_t e, const char* what);
+
 // a bulk append, sorted by bins of buckets (v.meta_new: v.meta_old)
 void launch_append_bins(const IndexView& v, const StepIn& in, const Bins& b, bool maybe_empty, hipStream_t st);
 
