@@ -1,13 +1,14 @@
 // csd — attention of all paths' new tokens over the cache: a wave's part of it.
 //
-// A wave holds QT tiles of 32 query rows as columns of S^T = K Q^T and O^T += V^T P^T, and goes through blocks of 32
-// tokens.  In that orientation a lane's registers belong to one query row (two lanes a row, one for each half of a
+// A wave holds a tile of 32 query rows as columns of S^T = K Q^T and O^T += V^T P^T, and goes through blocks of 32 tokens.
+// In that orientation a lane's registers belong to one query row (two lanes a row, one for each half of a
 // block's tokens), so the running maximum m and sum l of the softmax, in base 2, are a register each, and rescaling
 // O by 2^(m_old - m_new) needs no exchange; two lanes exchange one value per block for the maximum.
 //
-// 8-bit values are multiplied without their scales 2^e: the exponent is added to the score, x = s + e, so that
-// P = 2^(x - m) with m the maximum of x is at most 1 whatever the scales are (in half precision too), and l sums
-// P 2^-e.  Keys' scales go into the conversion to 16 bits, which takes a power of two a lane.
+// 8-bit values are multiplied without their scales 2^e, which go into P: P 2^e is as exact in bfloat16 as P.  Half precision
+// has not the range: there the exponent is added to the score, x = s + e, so that P = 2^(x - m) with m the maximum of x
+// is at most 1 whatever the scales are, and l sums P 2^-e.  Keys' scales go into the conversion to 16 bits, which takes a
+// power of two a lane.
 //
 // Sums, maxima and O are in 32 bits.  P is rounded to the 16-bit type, to nearest, for the second product (the matrix
 // cores take no other): the weights of a row have errors of either sign that are as small as the output's own rounding.
@@ -35,190 +36,207 @@ __device__ inline float both_sum(float x) {
 // The token of a block that register r (0 .. 15) of a lane's scores belongs to.
 __device__ __host__ constexpr int token_of(int r, int half) { return 16 * (r >> 3) + 8 * half + (r & 7); }
 
-// A block's keys or values as they lie in the cache, 16 bytes a lane and register.
+// A block in LDS: keys, values, and the scales of an 8-bit cache, as they lie in the cache.
 template <int D, bool FP8>
-struct Raw {
-  static constexpr int kLoads = FP8 ? D / 32 : D / 16;
-  Words at[kLoads];
-  __device__ void load(const uint8_t* block, int lane) {
-#pragma unroll
-    for (int c = 0; c < kLoads; ++c) at[c] = *reinterpret_cast<const Words*>(block + c * 1024 + lane * 16);
-  }
+struct Staged {
+  static constexpr int kHalf = kBlock * D * (FP8 ? 1 : 2);             // bytes of the keys
+  static constexpr int kBytes = 2 * kHalf + (FP8 ? kScaleBytes : 0);
+  const uint8_t* at;
+  __device__ Words keys(int c, int lane) const { return *reinterpret_cast<const Words*>(at + c * 1024 + lane * 16); }
+  __device__ Words values(int c, int lane) const { return *reinterpret_cast<const Words*>(at + kHalf + c * 1024 + lane * 16); }
+  __device__ const uint8_t* scales() const { return at + 2 * kHalf; }
 };
 
-template <class T, int D, bool FP8, int QT>
+template <class T, int D, bool FP8>
 struct Wave {
   typedef typename T::Eight Eight;
   static constexpr int kTiles = D / 32;                  // of O's rows
 
-  Acc o[QT][kTiles];
-  Eight q[QT][D / 16];
-  float m[QT], l[QT];                                    // of the lane's query row; l of its half of the tokens
-  int32_t sees[QT];                                      // tokens of the present segment that the row sees
-  float scale;                                           // times log2(e)
+  Acc o[kTiles];
+  Eight q[D / 16];
+  float m, l;                                            // of the lane's query row; l of its half of the tokens
+  float scale;                                           // times log2(e), positive: the queries take the sign, or are zero
   int lane, half;
 
   __device__ void begin(float scale_log2) {
     lane = threadIdx.x & 63;
     half = lane >> 5;
     // (a half-precision key of 8 bits times its scale may come out as 65536, so they are converted to half of it)
-    scale = scale_log2 * (FP8 && is_half() ? 2.0f : 1.0f);
+    scale = (scale_log2 == 0 ? 1.0f : fabsf(scale_log2)) * (FP8 && is_half() ? 2.0f : 1.0f);
+    m = kNone;
+    l = 0;
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      m[t] = kNone;
-      l[t] = 0;
-      sees[t] = 0;
-#pragma unroll
-      for (int x = 0; x < kTiles; ++x) o[t][x] = Acc{};
-    }
+    for (int x = 0; x < kTiles; ++x) o[x] = Acc{};
   }
   static constexpr bool is_half() { return T::kExponent == F16::kExponent; }
 
-  __device__ static Eight key_operand(const Raw<D, FP8>& k, int c, float key_scale) {
+  // S^T of a block
+  __device__ Acc scores(const Staged<D, FP8>& b) const {
+    Acc s{};
     if constexpr (FP8) {
-      const Words w = k.at[c / 2];
-      return from_fp8<T>(c & 1 ? Pair{w[2], w[3]} : Pair{w[0], w[1]}, key_scale);
-    } else {
-      return __builtin_bit_cast(Eight, k.at[c]);
-    }
-  }
-  // rows 32 x .., tokens 16 u ..; of those, tokens from `from` on are kept and those from `to` on are not (of the block)
-  template <bool EDGE>
-  __device__ Eight value_operand(const Raw<D, FP8>& v, int x, int u, int from, int to) const {
-    const int first = 16 * u + 8 * half;
-    if constexpr (FP8) {
-      Pair w = u ? Pair{v.at[x][2], v.at[x][3]} : Pair{v.at[x][0], v.at[x][1]};
-      if constexpr (EDGE) {
+      const float key_scale = __uint_as_float(((uint32_t)b.scales()[lane & 31] - (is_half() ? 1 : 0)) << 23);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (first + i < from || first + i >= to) w[i / 4] &= ~(0xffu << 8 * (i & 3));
+      for (int c = 0; c < D / 32; ++c) {
+        const Words w = b.keys(c, lane);
+        s = T::mfma(from_fp8<T>(Pair{w[0], w[1]}, key_scale), q[2 * c], s);
+        s = T::mfma(from_fp8<T>(Pair{w[2], w[3]}, key_scale), q[2 * c + 1], s);
       }
-      return from_fp8<T>(w, 1.0f);
     } else {
-      Words w = v.at[2 * x + u];
-      if constexpr (EDGE) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (first + i < from || first + i >= to) w[i / 2] &= ~(0xffffu << 16 * (i & 1));
-      }
-      return __builtin_bit_cast(Eight, w);
+      for (int c = 0; c < D / 16; ++c) s = T::mfma(__builtin_bit_cast(Eight, b.keys(c, lane)), q[c], s);
     }
-  }
-  // whether the lane holds an infinity or a NaN among the values of tokens from .. to - 1
-  __device__ bool odd_values(const Raw<D, FP8>& v, int from, int to) const {
-    bool odd = false;
-#pragma unroll
-    for (int x = 0; x < kTiles; ++x)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int token = 16 * u + 8 * half + i;
-          uint32_t bits;
-          if constexpr (FP8) bits = (v.at[x][2 * u + i / 4] >> 8 * (i & 3) & 0x7f) == 0x7f;
-          else bits = (v.at[2 * x + u][i / 2] >> 16 * (i & 1) & T::kExponent) == T::kExponent;
-          odd |= token >= from && token < to && bits;
-        }
-    return odd;
+    return s;
   }
 
-  // One block of 32 tokens, the first of which is token `first` of the segment.  EDGE: some row does not see all of them:
-  // from `all` on not all rows see a token, from `most` on none does (of the segment).  next(): the keys are free.
-  template <bool EDGE, class Next>
-  __device__ void block(const Raw<D, FP8>& k, const Raw<D, FP8>& v, const uint8_t* scales, int32_t first, int32_t all,
-                        int32_t most, Next next) {
-    Acc s[QT];
-    float key_scale = 1.0f;
-    if constexpr (FP8) key_scale = __uint_as_float(((uint32_t)scales[lane & 31] - (is_half() ? 1 : 0)) << 23);
-#pragma unroll
-    for (int t = 0; t < QT; ++t) s[t] = Acc{};
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) {
-      const Eight a = key_operand(k, c, key_scale);
-#pragma unroll
-      for (int t = 0; t < QT; ++t) s[t] = T::mfma(a, q[t][c], s[t]);
-    }
-    next();
-    softmax<EDGE>(s, scales, first);
-    Eight p[QT][2];
-#pragma unroll
-    for (int t = 0; t < QT; ++t)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[t][u][i] = (typename T::One)s[t][8 * u + i];
-    int to = 32;
-    if constexpr (EDGE) {
-      to = most - first;
-      const int from = all - first < 0 ? 0 : all - first;
-      // 0 x infinity would reach the rows that do not see the token: such tokens go one by one, to the rows that do
-      if (__ballot(odd_values(v, from, to))) {
-        for (int token = from; token < to && token < kBlock; ++token) {
-#pragma unroll
-          for (int x = 0; x < kTiles; ++x) {
-            const Eight v0 = value_operand<true>(v, x, 0, token, token + 1), v1 = value_operand<true>(v, x, 1, token, token + 1);
-#pragma unroll
-            for (int t = 0; t < QT; ++t) {
-              const Acc one = T::mfma(v1, p[t][1], T::mfma(v0, p[t][0], Acc{}));
-              const bool seen = first + token < sees[t];
-#pragma unroll
-              for (int r = 0; r < 16; ++r) o[t][x][r] += seen ? one[r] : 0.0f;
-            }
-          }
-        }
-        to = from;
-      }
-    }
-#pragma unroll
-    for (int x = 0; x < kTiles; ++x)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const Eight a = value_operand<EDGE>(v, x, u, 0, to);
-#pragma unroll
-        for (int t = 0; t < QT; ++t) o[t][x] = T::mfma(a, p[t][u], o[t][x]);
-      }
-  }
-
-  // Scores to weights, with the running maximum and sum.
+  // Scores to weights (times their values' scales), with the running maximum and sum.  EDGE: the row sees the block's first `sees`
+  // tokens.
   template <bool EDGE>
-  __device__ void softmax(Acc (&s)[QT], const uint8_t* scales, int32_t first) {
+  __device__ void softmax(Acc& s, const Staged<D, FP8>& b, int32_t sees) {
     uint32_t exps[4];                                    // of the lane's 16 tokens' values
     if constexpr (FP8) {
-      const Pair lo = *reinterpret_cast<const Pair*>(scales + kBlock + 8 * half), hi = *reinterpret_cast<const Pair*>(scales + kBlock + 16 + 8 * half);
+      const Pair lo = *reinterpret_cast<const Pair*>(b.scales() + kBlock + 8 * half), hi = *reinterpret_cast<const Pair*>(b.scales() + kBlock + 16 + 8 * half);
       exps[0] = lo[0], exps[1] = lo[1], exps[2] = hi[0], exps[3] = hi[1];
     }
     auto exponent = [&](int r) { return exps[r / 4] >> 8 * (r & 3) & 0xff; };
+    constexpr bool kAdded = FP8 && is_half();
+    float most = kNone;
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      float most = kNone;
+    for (int r = 0; r < 16; ++r) {
+      if constexpr (kAdded) s[r] = fmaf(s[r], scale, (float)exponent(r) - 127.0f);
+      if constexpr (EDGE) s[r] = token_of(r, half) < sees ? s[r] : kNone;
+      most = fmaxf(most, s[r]);
+    }
+    most = fmaxf(m, kAdded ? both_max(most) : both_max(most) * scale);
+    if (__ballot(most > m)) {                            // (m -inf: nothing has been summed)
+      const float down = m == kNone ? 0.0f : exp2_fast(m - most);
+      l *= down;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float x = s[t][r] * scale;
-        if constexpr (FP8) x = fmaf(s[t][r], scale, (float)exponent(r) - 127.0f);
-        if constexpr (EDGE) x = first + token_of(r, half) < sees[t] ? x : kNone;
-        s[t][r] = x;
-        most = fmaxf(most, x);
+      for (int x = 0; x < kTiles; ++x) o[x] *= down;
+      m = most;
+    }
+    const float base = m == kNone ? 0.0f : m;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = exp2_fast(kAdded ? s[r] - base : fmaf(s[r], scale, -base));
+      if constexpr (!FP8) {
+        l += s[r];
+      } else if constexpr (kAdded) {
+        const float up = __uint_as_float((254 - exponent(r)) << 23);
+        if constexpr (EDGE) l += token_of(r, half) < sees ? s[r] * up : 0.0f;
+        else l = fmaf(s[r], up, l);
+      } else {
+        l += s[r];
+        const float up = __uint_as_float(exponent(r) << 23);
+        if constexpr (EDGE) s[r] = token_of(r, half) < sees ? s[r] * up : 0.0f;
+        else s[r] *= up;
       }
-      most = fmaxf(m[t], both_max(most));
-      if (__ballot(most > m[t])) {                       // (m -inf: nothing has been summed)
-        const float down = m[t] == kNone ? 0.0f : exp2_fast(m[t] - most);
-        l[t] *= down;
+    }
+  }
+
+  __device__ static Eight value_operand(Words w, int u) {
+    if constexpr (FP8) return from_fp8<T>(u ? Pair{w[2], w[3]} : Pair{w[0], w[1]}, 1.0f);
+    else return __builtin_bit_cast(Eight, w);
+  }
+  static constexpr int value_load(int x, int u) { return FP8 ? x : 2 * x + u; }
+  // the bits of the first `to` tokens of the block in the operand of tokens 16 u ..
+  __device__ Words kept(int u, int to) const {
+    const int n = to - 16 * u - 8 * half;                // of the operand's eight
+    auto below = [](int bits) { return bits <= 0 ? 0ull : bits >= 64 ? ~0ull : (1ull << bits) - 1; };
+    Words w{};
+    const uint64_t low = below(n * (FP8 ? 8 : 16)), high = FP8 ? 0 : below(n * 16 - 64);
+    w[FP8 ? 2 * u : 0] = (uint32_t)low, w[FP8 ? 2 * u + 1 : 1] = (uint32_t)(low >> 32);
+    if constexpr (!FP8) w[2] = (uint32_t)high, w[3] = (uint32_t)(high >> 32);
+    return w;
+  }
+  // all bits of the values that are an infinity or a NaN: whose exponent (8 bits: all but the sign) is all ones
+  __device__ static Words odd(Words w) {
+    constexpr uint32_t kOnes = FP8 ? 0x7f7f7f7f : T::kExponent * 0x10001u, kLow = FP8 ? 0x01010101 : (T::kExponent & ~(T::kExponent << 1)) * 0x10001u;
 #pragma unroll
-        for (int x = 0; x < kTiles; ++x) o[t][x] *= down;
-        m[t] = most;
-      }
-      const float base = m[t] == kNone ? 0.0f : m[t];
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t top = ((w[i] & kOnes) + kLow) & (FP8 ? 0x80808080 : 0x80008000);
+      w[i] = top | (top - (top >> (FP8 ? 7 : 15)));
+    }
+    return w;
+  }
+
+  __device__ static void weights(const Acc& s, Eight (&p)[2]) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float w = exp2_fast(s[t][r] - base);
-        s[t][r] = w;
-        if constexpr (FP8) {
-          const float up = __uint_as_float((254 - exponent(r)) << 23);
-          if constexpr (EDGE) l[t] += first + token_of(r, half) < sees[t] ? w * up : 0.0f;
-          else l[t] = fmaf(w, up, l[t]);
-        } else {
-          l[t] += w;
+    for (int r = 0; r < 16; ++r) p[r / 8][r & 7] = (typename T::One)s[r];
+  }
+
+  // O^T += V^T P^T.  EDGE: from token `all` of the block on some of the wave's rows do not see a token, from `most` on none does.
+  // 0 x infinity would reach the rows that do not see a token, so infinities and NaN of such tokens are left to odd_values();
+  // returned is whether the lane has met any.
+  template <bool EDGE>
+  __device__ bool values(const Acc& s, const Staged<D, FP8>& b, int32_t all, int32_t most) {
+    Eight p[2];
+    weights(s, p);
+    if constexpr (EDGE) {
+      all = all < 0 ? 0 : all;
+      if (all < most && all < kBlock) {
+        const Words sure[2] = {kept(0, all), kept(1, all)}, seen[2] = {kept(0, most), kept(1, most)};
+        uint32_t met = 0;
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x) {
+          Words w{};
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            if (u == 0 || !FP8) w = b.values(value_load(x, u), lane);
+            const Words strange = odd(w) & seen[u] & ~sure[u];
+            met |= strange[0] | strange[1] | strange[2] | strange[3];
+            o[x] = T::mfma(value_operand(w & seen[u] & ~strange, u), p[u], o[x]);
+          }
         }
+        return met != 0;
+      }
+    }
+    const Words seen[2] = {kept(0, EDGE ? most : kBlock), kept(1, EDGE ? most : kBlock)};
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) {
+      Words w{};
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (u == 0 || !FP8) w = b.values(value_load(x, u), lane);
+        o[x] = T::mfma(value_operand(EDGE ? w & seen[u] : w, u), p[u], o[x]);
+      }
+    }
+    return false;
+  }
+  // What values() has left out of a block, which is read from memory again: one token after the other, for the rows that see it.
+  __device__ void odd_values(const uint8_t* block, const uint8_t* scales, int32_t sees, int32_t all, int32_t most) {
+    Acc s{};
+    const Staged<D, FP8> b{block};
+    float key_scale = 1.0f;
+    if constexpr (FP8) key_scale = __uint_as_float(((uint32_t)scales[lane & 31] - (is_half() ? 1 : 0)) << 23);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+      if constexpr (FP8) {
+        const Words w = b.keys(c / 2, lane);
+        s = T::mfma(from_fp8<T>(c & 1 ? Pair{w[2], w[3]} : Pair{w[0], w[1]}, key_scale), q[c], s);
+      } else {
+        s = T::mfma(__builtin_bit_cast(Eight, b.keys(c, lane)), q[c], s);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const uint32_t exponent = FP8 ? scales[kBlock + token_of(r, half)] : 127;
+      const float added = FP8 && is_half() ? (float)exponent - 127.0f : 0.0f, times = FP8 && !is_half() ? __uint_as_float(exponent << 23) : 1.0f;
+      s[r] = token_of(r, half) < sees ? exp2_fast(fmaf(s[r], scale, added) - (m == kNone ? 0.0f : m)) * times : 0.0f;
+    }
+    Eight p[2];
+    weights(s, p);
+    for (int32_t token = all < 0 ? 0 : all; token < most && token < kBlock; ++token) {
+      const Words alone[2] = {kept(0, token + 1) & ~kept(0, token), kept(1, token + 1) & ~kept(1, token)};
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x) {
+        Acc one{};
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const Words w = b.values(value_load(x, u), lane);
+          one = T::mfma(value_operand(w & odd(w) & alone[u], u), p[u], one);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[x][r] += token < sees ? one[r] : 0.0f;
       }
     }
   }

@@ -1,12 +1,14 @@
-// csd — attention of few query rows: its kernels.
+// csd — attention of all paths' new tokens over the cache: its kernels.
 //
-// attend_rows_kernel: a workgroup takes one tile of 32 QT query rows of a kv head and a run of blocks of 32 tokens, which its
-// waves share out among each other; every wave reads its blocks straight into registers (1 KB a load, no LDS: nothing is used
-// twice), and the waves' sums are joined in LDS.
-//   DIRECT: the rows are one path's, the run is the whole prompt and then the path: the result is written at once.
-//   else:   the rows are one path's and the run a part of its own tokens, or they are all paths' of a problem, without
-//           gaps for tokens beyond the paths' counts, and the run a part of the prompt: O / l and lse of each part are
-//           written in 32 bits and attend_join_kernel weighs them by 2^lse.
+// attend_rows_kernel: an item is a tile of up to 128 query rows of a kv head and a run of blocks of 32 tokens.  The four waves
+// of a workgroup take 32 rows each and share the blocks; where there are fewer rows, two waves (or all four) have the same rows,
+// take every second (fourth) block, and their sums are joined in LDS.  Blocks go from memory straight to a ring of
+// stages in LDS, several ahead of the products; a wave waits for its own loads by their count, and waves that share
+// a block meet at barriers.  The rows are
+//   of one path, and the run is a part of its own tokens (kDirect: the whole prompt, then the path), or
+//   of all paths of a problem, without gaps for tokens beyond the paths' counts, and the run is a part of the prompt.
+// Results are written at once where an item has seen all that its rows see, else as a part of each row, O / l and lse
+// in 32 bits, and attend_join_kernel (kFinal: the path's item) weighs the parts by 2^lse.
 #pragma once
 
 #include "csd_attend.cuh"
@@ -14,13 +16,7 @@
 namespace csd {
 namespace verify {
 
-constexpr int kRowWaves = 4;
-
-// The tokens that the query rows of a tile are of, G rows each: the tile's first row is of slot 0.
-template <int QT>
-struct Slots {
-  int32_t token[32 * QT + 1];            // i n + t, -1: none
-};
+constexpr int kWaves = 4, kWide = 32 * kWaves;
 
 template <class T>
 __device__ inline void store8(void* out, int64_t at, const float (&x)[8]) {
@@ -32,13 +28,17 @@ __device__ inline void store8(void* out, int64_t at, const float (&x)[8]) {
 
 __device__ inline int32_t clamped(int32_t x, int32_t most) { return x < 0 ? 0 : x > most ? most : x; }
 
+// The tokens that the query rows of a tile are of, G rows each: the tile's first row is of slot 0.
+struct Slots {
+  int32_t token[kWide + 1];              // i n + t, -1: none
+};
+
 // Puts the tokens of all paths of problem p, counts[i] each, behind each other, and takes those from `first` on.  Returns how
 // many there are in all.  One wave calls it.
-template <int QT>
-__device__ int32_t pack_tokens(const AttendArgs& a, int32_t p, int32_t first, Slots<QT>* slots) {
+__device__ inline int32_t pack_tokens(const AttendArgs& a, int32_t p, int32_t first, Slots* slots) {
   const int lane = threadIdx.x & 63;
-  constexpr int kWide = 32 * QT + 1;
-  for (int x = lane; x < kWide; x += 64) slots->token[x] = -1;
+  constexpr int kSlots = kWide + 1;
+  for (int x = lane; x < kSlots; x += 64) slots->token[x] = -1;
   const int32_t* counts = a.counts ? a.counts + (int64_t)p * a.N : nullptr;
   int32_t before = 0;
   for (int32_t i0 = 0; i0 < a.N; i0 += 64) {
@@ -51,207 +51,442 @@ __device__ int32_t pack_tokens(const AttendArgs& a, int32_t p, int32_t first, Sl
       if (lane >= d) sum += other;
     }
     const int32_t at = before + sum - mine - first;      // the slot of the path's first token
-    const int32_t end = mine < kWide - at ? mine : kWide - at;
+    const int32_t end = mine < kSlots - at ? mine : kSlots - at;
     for (int32_t t = at < 0 ? -at : 0; t < end; ++t) slots->token[at + t] = i * a.n + t;
     before += __shfl(sum, 63);
   }
   return before;
 }
 
-// blocks of tokens [from, to) of the segment that lies at `held`, dealt to the waves
-template <class W, int D, bool FP8>
-__device__ inline void stream(W& w, const Held& held, int64_t first_block, int32_t from, int32_t to, int32_t turn, int32_t turns,
-                              int32_t all, int32_t most) {
-  const uint8_t* const data = held.data + first_block * held.block_bytes;
-  const uint8_t* const scale = FP8 ? held.scale + first_block * kScaleBytes : nullptr;
-  constexpr int64_t kBytes = block_bytes(D, FP8);
-  int32_t b = from + turn;
-  if (b >= to) return;
-  Raw<D, FP8> k, v;
-  k.load(data + b * kBytes, w.lane);
-  while (true) {
-    v.load(data + b * kBytes + kBytes / 2, w.lane);
-    const int32_t then = b + turns;
-    auto next = [&] {
-      if (then < to) k.load(data + then * kBytes, w.lane);
-    };
-    const int32_t first = b * kBlock;
-    if (first + kBlock <= all) w.template block<false>(k, v, scale + (FP8 ? (int64_t)b * kScaleBytes : 0), first, all, most, next);
-    else w.template block<true>(k, v, scale + (FP8 ? (int64_t)b * kScaleBytes : 0), first, all, most, next);
-    if (then >= to) return;
-    b = then;
-  }
+// ---- loads to LDS.  The first wait is for the wave's own reads of the stage that is written.
+
+// (the same for all lanes: in scalar registers, whatever the compiler can tell)
+__device__ inline uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ inline const uint8_t* uniform(const uint8_t* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  const uint32_t low = uniform((uint32_t)x), high = uniform((uint32_t)(x >> 32));
+  return reinterpret_cast<const uint8_t*>((uint64_t)high << 32 | (uint64_t)low);
 }
 
-template <class T, int D, bool FP8, int QT, bool DIRECT>
-__global__ __launch_bounds__(64 * kRowWaves, QT == 1 && D <= 128 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
-  constexpr int kWide = 32 * QT, kChunk = D % 64 == 0 ? 64 : 32;
-  __shared__ Slots<QT> slots;
-  __shared__ int32_t total;
-  __shared__ float tops[kRowWaves][32], sums[kRowWaves][32];
-  __shared__ alignas(16) float parts[kRowWaves][32][kChunk + 4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// N pieces of 1 KB, a lane's 16 bytes at from + piece KB + 16 lane
+template <int N>
+__device__ inline void fetch(uint32_t lds, const uint8_t* from, uint32_t lane_bytes) {
+  if constexpr (N >= 4) {
+    asm volatile(
+        "s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
+        "global_load_lds_dwordx4 %1, %2 offset:1024\n\tglobal_load_lds_dwordx4 %1, %2 offset:2048\n\t"
+        "global_load_lds_dwordx4 %1, %2 offset:3072" ::"s"(lds), "v"(lane_bytes), "s"(from) : "memory");
+    if constexpr (N > 4) fetch<N - 4>(lds + 4096, from + 4096, lane_bytes);
+  } else if constexpr (N >= 2) {
+    asm volatile(
+        "s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
+        "global_load_lds_dwordx4 %1, %2 offset:1024" ::"s"(lds), "v"(lane_bytes), "s"(from) : "memory");
+    if constexpr (N > 2) fetch<N - 2>(lds + 2048, from + 2048, lane_bytes);
+  } else {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_bytes), "s"(from) : "memory");
+  }
+}
+// 64 bytes, 4 from each of the first sixteen lanes
+__device__ inline void fetch_scales(uint32_t lds, const uint8_t* from, int lane) {
+  if (lane < 16)
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(lane * 4), "s"(from) : "memory");
+}
+// until no more than N of the wave's loads are under way
+template <int N>
+__device__ inline void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N < 63 ? N : 63) : "memory");   // (it counts no further)
+}
+__device__ inline void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+__device__ inline uint32_t lds_offset(const void* p) {
+  return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p);
+}
+
+// The sizes of a ring: stages for two workgroups on a CU, where a stage for each wave leaves room for them.
+template <int D, bool FP8>
+struct Ring {
+  typedef Staged<D, FP8> Stage;
+  static constexpr int kKeys = Stage::kHalf / 1024;      // pieces of the keys, and of the values
+  static constexpr int stages() {
+    int x = kWaves;
+    while (x * 2 * Stage::kBytes <= 72 * 1024) x *= 2;
+    return x;
+  }
+  static constexpr int kStages = stages();
+  static constexpr int kBytes = kStages * Stage::kBytes;
+  static constexpr int kResident = kBytes <= 72 * 1024 && D <= 128 ? 2 : 1;   // workgroups of a CU
+  // loads of a wave when C waves share them
+  template <int C>
+  static constexpr int pieces() { return (kKeys + C - 1) / C; }
+
+  // The wave's share of the keys (and scales), of the values
+  template <int C>
+  static __device__ void keys(uint32_t lds, const uint8_t* block, const uint8_t* scale, int group, int lane) {
+    constexpr int N = pieces<C>();
+    const uint32_t first = 1024u * (group * N < kKeys - N ? group * N : kKeys - N);
+    fetch<N>(uniform(lds + first), uniform(block + first), lane * 16);
+    if constexpr (FP8) fetch_scales(uniform(lds + 2 * Stage::kHalf), uniform(scale), lane);
+  }
+  template <int C>
+  static __device__ void values(uint32_t lds, const uint8_t* block, int group, int lane) {
+    constexpr int N = pieces<C>();
+    const uint32_t first = Stage::kHalf + 1024u * (group * N < kKeys - N ? group * N : kKeys - N);
+    fetch<N>(uniform(lds + first), uniform(block + first), lane * 16);
+  }
+};
+
+// A run of blocks: the prompt's and the path's that all rows of the tile see whole, then those that some row does not see
+// all of.
+struct Segment {
+  const uint8_t *data, *scale;           // of its first block in the run
+  int32_t first, whole, edge;            // the first block's number, how many blocks are seen whole, how many follow them
+};
+struct Run {
+  Segment prompt, path;
+  __device__ int32_t whole() const { return prompt.whole + path.whole; }
+  __device__ int32_t blocks() const { return whole() + prompt.edge + path.edge; }
+  // the run's x-th block: which of its segment's
+  __device__ int32_t place(int32_t x, bool* of_path) const {
+    const bool edge = x >= whole();
+    if (edge) x -= whole();
+    const int32_t before = edge ? prompt.edge : prompt.whole;
+    *of_path = x >= before;
+    if (*of_path) x -= before;
+    return edge ? x + (*of_path ? path.whole : prompt.whole) : x;
+  }
+};
+
+// Goes through the run's blocks turn, turn + turns, ..; C waves have the same blocks, the wave is the `group`th, and their share of the
+// ring is at `ring`.  prompt_len, sees: tokens of the prompt, of the path that the lane's row sees; all, most: of the path,
+// that all of the wave's rows, that any of them sees.  queries() loads the wave's queries, while the first blocks are on their way.
+// Returns whether there are values left for odd_values().
+template <class T, int D, bool FP8, int C, class Queries>
+__device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, const uint8_t* ring, int32_t group, int32_t turn, int32_t turns,
+                              int32_t prompt_len, int32_t sees, int32_t all, int32_t most, Queries queries) {
+  typedef Ring<D, FP8> R;
+  constexpr int64_t kBlockBytes = 2 * R::Stage::kHalf;
+  constexpr bool kShared = C > 1;
+  constexpr int kStages = R::kStages / kWaves * C;
+  const uint32_t lds = uniform(lds_offset(ring));
+  const int32_t whole = run.whole(), blocks = run.blocks();
+  const int32_t mine = blocks > turn ? (blocks - turn + turns - 1) / turns : 0;
+  const int32_t rounds = kShared ? (blocks + turns - 1) / turns : mine;       // (all waves meet equally often)
+  auto load_keys = [&](int32_t j, int32_t stage) {
+    bool path;
+    const int64_t at = run.place(turn + j * turns, &path);
+    R::template keys<C>(lds + stage * R::Stage::kBytes, (path ? run.path.data : run.prompt.data) + at * kBlockBytes,
+                        (path ? run.path.scale : run.prompt.scale) + (FP8 ? at * kScaleBytes : 0), group, w.lane);
+  };
+  auto load_values = [&](int32_t j, int32_t stage) {
+    bool path;
+    const int64_t at = run.place(turn + j * turns, &path);
+    R::template values<C>(lds + stage * R::Stage::kBytes, (path ? run.path.data : run.prompt.data) + at * kBlockBytes, group, w.lane);
+  };
+  // until the loads before the newest (kStages - 1) * kLoads + MORE are done, if so many have been issued behind them
+  constexpr int kKeyLoads = R::template pieces<C>() + (FP8 ? 1 : 0), kValueLoads = R::template pieces<C>();
+  constexpr int kBehind = (kStages - 1) * (kKeyLoads + kValueLoads);
+  auto wait = [&](bool behind, auto more) {
+    if (behind) wait_loads<kBehind + decltype(more)::value>();
+    else wait_loads<0>();
+  };
+  for (int32_t j = 0; j < kStages && j < mine; ++j) {
+    load_keys(j, j);
+    if (!kShared || j < kStages - 1) load_values(j, j);
+  }
+  queries();
+  // (with the builtin, so that the compiler knows: it would wait for the queries, and so for all loads, in every round)
+  __builtin_amdgcn_s_waitcnt(0x0f70);                    // vmcnt(0)
+  int32_t stage = 0;
+  bool met = false;
+  auto round = [&](int32_t j, auto edge_of) {
+    constexpr bool kEdge = decltype(edge_of)::value;
+    const bool here = j < mine;
+    const typename R::Stage b{ring + stage * R::Stage::kBytes};
+    bool path = false;
+    int32_t first = 0;
+    if constexpr (kEdge) {
+      const int32_t at = run.place(turn + j * turns, &path);
+      first = kBlock * (at + (path ? run.path.first : run.prompt.first));
+    }
+    Acc s;
+    wait(j + kStages - 1 < mine, std::integral_constant<int, kShared ? 0 : kValueLoads>{});
+    if constexpr (kShared) {
+      meet();                                            // the keys are there, and all are done with the last block's values
+      if (j + kStages - 1 < mine) load_values(j + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+    }
+    if (here) {
+      s = w.scores(b);
+      w.template softmax<kEdge>(s, b, (path ? sees : prompt_len) - first);
+    }
+    if constexpr (kShared) {
+      wait(j + kStages - 1 < mine, std::integral_constant<int, 0>{});
+      meet();                                            // the values are there, and all are done with the keys
+      if (j + kStages < mine) load_keys(j + kStages, stage);
+    } else {
+      // (the scales, which lie behind the keys, have been read by then)
+      if (j + kStages < mine) load_keys(j + kStages, stage);
+      wait(j + kStages < mine, std::integral_constant<int, kKeyLoads>{});
+    }
+    if (here) met |= w.template values<kEdge>(s, b, (path ? all : prompt_len) - first, (path ? most : prompt_len) - first);
+    if constexpr (!kShared) {
+      if (j + kStages < mine) load_values(j + kStages, stage);
+    }
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+  };
+  int32_t j = 0;
+  for (; j < rounds && turn + j * turns < whole; ++j) round(j, std::false_type{});
+  for (; j < rounds; ++j) round(j, std::true_type{});
+  return __ballot(met) != 0;
+}
+
+// Makes what the lanes of a wave have written to LDS visible to each other.
+__device__ inline void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+template <class T, int D, bool FP8>
+__global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend_rows_kernel(AttendArgs a) {
+  constexpr int kChunk = D % 64 == 0 ? 64 : 32, kMine = kChunk / 8;
+  typedef typename T::One One;
+  typedef typename T::Eight Eight;
+  typedef Ring<D, FP8> R;
+  typedef float Part[kChunk + 4];                        // a row's sums of a chunk of d's
+  static_assert(sizeof(Part) * 32 <= R::kBytes / kWaves && R::kBytes / kWaves % 16 == 0);
+  __shared__ Slots slots;
+  __shared__ int32_t packed;
+  __shared__ float tops[kWaves][32], sums[kWaves][32], lses[kWaves][32];
+  __shared__ int32_t places[kWaves][32];
+  __shared__ alignas(16) uint8_t ring[R::kBytes];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // the item
+  const bool prompt = (int32_t)blockIdx.x < a.prompt_groups;
+  const bool solo = !prompt && a.solo, results = !prompt && a.how != kParts;
   uint32_t item = blockIdx.x;
-  const uint32_t prompt_items = DIRECT ? 0 : (uint32_t)a.P * a.Hk * a.prompt_splits * a.prompt_tiles;
-  const bool prompt = item < prompt_items;
-  if (!prompt) item -= prompt_items;
-  const uint32_t tiles = prompt ? a.prompt_tiles : a.path_tiles, splits = DIRECT ? 1 : prompt ? a.prompt_splits : a.path_splits;
-  const int32_t tile = item % tiles;
-  item /= tiles;
+  if (!prompt) item -= a.prompt_groups;
+  if (solo) item = item * kWaves + wave;
+  // `inner` items that have tokens in common lie behind each other, or, as workgroups are dealt to the eight XCDs in turn, eight
+  // items apart
+  const uint32_t inner = prompt ? a.prompt_tiles : a.how == kDirect ? a.N * a.path_tiles : a.path_tiles;
+  const uint32_t outer = prompt ? (uint32_t)a.P * a.Hk * a.prompt_splits : a.how == kDirect ? (uint32_t)a.P * a.Hk : (uint32_t)a.P * a.N * a.Hk * a.path_splits;
+  uint32_t within;
+  if (prompt ? a.prompt_turns : a.path_turns) {
+    const uint32_t turn = item / 8;
+    within = turn % inner;
+    item = turn / inner * 8 + item % 8;
+  } else {
+    within = item % inner;
+    item /= inner;
+  }
+  if (item >= outer) return;
+  const uint32_t splits = prompt ? a.prompt_splits : a.path_splits;
   const int32_t split = item % splits;
   item /= splits;
   const int32_t head = item % a.Hk;
-  const int64_t row = item / a.Hk;                       // problem, or problem and path
-  const int32_t p = prompt ? row : row / a.N;
+  item /= a.Hk;
+  int32_t tile = within, p = item, i = 0;
+  if (!prompt) {
+    if (a.how == kDirect) {
+      i = within / (uint32_t)a.path_tiles;
+      tile = within % (uint32_t)a.path_tiles;
+    } else {
+      p = item / (uint32_t)a.N;
+      i = item % (uint32_t)a.N;
+    }
+  }
+  const int64_t row = prompt ? p : (int64_t)p * a.N + i;
 
+  const int32_t wide = solo ? 32 : kWide;
   const int32_t prompt_len = a.prompt.cap ? (a.prompt_len ? clamped(a.prompt_len[p], a.prompt.cap) : a.prompt.cap) : 0;
   int32_t count = 0, path_len = 0;
   if (!prompt) {
     count = a.counts ? clamped(a.counts[row], a.n) : a.n;
     path_len = clamped(a.path_len[row], a.path.cap);
   }
-  const int32_t first = tile * kWide, first_token = first / a.G;
+  const int32_t first = tile * wide, first_token = first / a.G;
+  int32_t total = count * a.G;                           // of the rows that are there
   if (prompt) {
     if (wave == 0) {
-      const int32_t all = pack_tokens<QT>(a, p, first_token, &slots);
-      if (lane == 0) total = all * a.G;
-    }
-  } else {
-    const int32_t i = (int32_t)(row - (int64_t)p * a.N), all = DIRECT ? a.n : count;
-    for (int x = threadIdx.x; x < kWide + 1; x += blockDim.x) slots.token[x] = first_token + x < all ? i * a.n + first_token + x : -1;
-    if (threadIdx.x == 0) total = all * a.G;
-  }
-  __syncthreads();
-  if (first >= total) return;
-
-  // the rows' queries
-  Wave<T, D, FP8, QT> w;
-  w.begin(a.scale);
-  const int64_t problem = (int64_t)p * a.N * a.n;        // its first token
-  int32_t least = INT32_MAX, most = 0;                   // of what the rows see of the path
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int32_t q_row = first + 32 * t + (lane & 31), g = q_row % a.G;
-    const int32_t token = slots.token[q_row / a.G - first_token];
-    const int32_t behind = token - (int32_t)(row - (int64_t)p * a.N) * a.n;   // path: its place among the new ones
-    const bool valid = token >= 0 && (prompt || behind < count);
-    if (!prompt && valid) {
-      w.sees[t] = clamped(path_len - count + behind + 1, path_len);
-      least = w.sees[t] < least ? w.sees[t] : least;
-      most = w.sees[t] > most ? w.sees[t] : most;
-    }
-    const int32_t path = token / a.n;
-    const auto* from = static_cast<const typename T::One*>(a.q.data) + ((int64_t)p * a.N + path) * a.q.row_stride + (int64_t)(token - path * a.n) * a.q.token_stride + (head * a.G + g) * a.q.head_stride;
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) {
-      w.q[t][c] = typename T::Eight{};
-      if (valid) w.q[t][c] = *reinterpret_cast<const typename T::Eight*>(from + 16 * c + 8 * w.half);
-    }
-  }
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    const int32_t x = __shfl_xor(least, d), y = __shfl_xor(most, d);
-    least = x < least ? x : least;
-    most = y > most ? y : most;
-  }
-  least = __builtin_amdgcn_readfirstlane(least);
-  most = __builtin_amdgcn_readfirstlane(most);
-
-  // its tokens
-  const int32_t prompt_blocks = (prompt_len + kBlock - 1) / kBlock, path_blocks = (most + kBlock - 1) / kBlock;
-  int32_t turn = wave;
-  if (DIRECT || prompt) {
-    int32_t path_sees[QT];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      path_sees[t] = w.sees[t];
-      w.sees[t] = prompt_len;
-    }
-    const int32_t per = (prompt_blocks + (int32_t)splits - 1) / (int32_t)splits;
-    const int32_t from = split * per, to = from + per < prompt_blocks ? from + per : prompt_blocks;
-    if (!DIRECT || count > 0)
-      stream<Wave<T, D, FP8, QT>, D, FP8>(w, a.prompt, a.prompt.first(p, head, a.Hk), from, to, turn, kRowWaves, prompt_len, prompt_len);
-#pragma unroll
-    for (int t = 0; t < QT; ++t) w.sees[t] = path_sees[t];
-    // the waves go on in turn
-    turn = (wave + kRowWaves - prompt_blocks % kRowWaves) % kRowWaves;
-  }
-  if (!prompt) {
-    const int32_t per = (path_blocks + (int32_t)splits - 1) / (int32_t)splits;
-    const int32_t from = split * per, to = from + per < path_blocks ? from + per : path_blocks;
-    stream<Wave<T, D, FP8, QT>, D, FP8>(w, a.path, a.path.first(row, head, a.Hk), from, to, turn, kRowWaves, least, most);
-  }
-
-  // the waves' sums joined
-  const int col = threadIdx.x / 8, part = threadIdx.x & 7;             // eight threads a row, kChunk / 8 values each
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const float own = both_sum(w.l[t]);
-    if (lane < 32) {
-      tops[wave][lane] = w.m[t];
-      sums[wave][lane] = own;
+      const int32_t all = pack_tokens(a, p, first_token, &slots);
+      if (lane == 0) packed = all;
     }
     __syncthreads();
-    auto join = [&](int c, float* top) {
-      float high = kNone, sum = 0;
-#pragma unroll
-      for (int x = 0; x < kRowWaves; ++x) high = fmaxf(high, tops[x][c]);
-#pragma unroll
-      for (int x = 0; x < kRowWaves; ++x) sum += sums[x][c] * (tops[x][c] == kNone ? 0.0f : exp2_fast(tops[x][c] - high));
-      *top = high;
-      return sum;
-    };
-    float top;
-    join(lane & 31, &top);
-    const float weight = w.m[t] == kNone ? 0.0f : exp2_fast(w.m[t] - top);
-    const float all = join(col, &top);
-    const int32_t q_row = first + 32 * t + col;
-    const int32_t token = slots.token[q_row / a.G - first_token];
-    const float sum = DIRECT && q_row >= count * a.G ? 0.0f : all;      // (of a token beyond the path's count: nothing)
-    const float over = 1.0f / sum;
-    const int64_t to = (problem + token) * a.H + head * a.G + q_row % a.G;
-    const int64_t place = (int64_t)(prompt ? split : a.prompt_splits + split) * a.rows + to;   // of a part
-    if (token >= 0 && part == 0) {
-      const float lse = sum == 0.0f ? kNone : top + __builtin_amdgcn_logf(sum);
-      if constexpr (!DIRECT) a.part_lse[place] = lse;
-      else if (a.lse) a.lse[to] = lse * 0.693147180559945309f;
+    total = __builtin_amdgcn_readfirstlane(packed) * a.G;
+  }
+  const int32_t here = total - first < wide ? total - first : wide;
+
+  if (results && first + wide > total && a.n * a.G > total) {                          // tokens beyond the path's count: zeros
+    const int32_t from = total > first ? total : first, end = a.n * a.G < first + wide ? a.n * a.G : first + wide;
+    for (int32_t x = from * (D / 8) + (solo ? lane : threadIdx.x); x < end * (D / 8); x += solo ? 64 : 64 * kWaves) {
+      const int32_t q_row = x / (D / 8), nth = (uint32_t)q_row / (uint32_t)a.G;
+      const int64_t to = (row * a.n + nth) * a.H + head * a.G + (q_row - nth * a.G);
+      *reinterpret_cast<Words*>(static_cast<One*>(a.out) + to * D + x % (D / 8) * 8) = Words{};
+      if (a.lse && x % (D / 8) == 0) a.lse[to] = kNone;
     }
+  }
+  if (here <= 0) return;
+
+  // groups of 32 rows, and the waves of each
+  const int32_t groups = solo || here <= 32 ? 1 : here <= 64 ? 2 : kWaves;
+  const int32_t turns = solo ? 1 : kWaves / groups, group = solo ? 0 : wave % groups, turn = solo ? 0 : wave / groups;
+
+  // the wave's queries
+  Wave<T, D, FP8> w;
+  w.begin(a.scale);
+  const int32_t own_row = first + 32 * group + (lane & 31);
+  int32_t sees = 0, all = INT32_MAX, most = 0;           // tokens of the path
+  const bool valid = own_row < total;
+  const int32_t nth = (uint32_t)own_row / (uint32_t)a.G, g = own_row - nth * a.G;      // its token in the item, its head of the group
+  int32_t path_of = i, t = nth;
+  if (prompt && valid) {
+    const int32_t token = slots.token[nth - first_token];
+    path_of = (uint32_t)token / (uint32_t)a.n;
+    t = token - path_of * a.n;
+  }
+  const int32_t own_place = ((path_of * a.n + t) * a.Hk + head) * a.G + g;             // the row of the problem's N n H
+  if (!prompt && valid) sees = all = most = clamped(path_len - count + nth + 1, path_len);
+  auto queries = [&] {
+    const One* from = static_cast<const One*>(a.q.data) + ((int64_t)p * a.N + path_of) * a.q.row_stride + t * a.q.token_stride + (head * a.G + g) * a.q.head_stride;
+    const uint32_t flip = a.scale < 0 ? 0x80008000u : 0u;
 #pragma unroll
-    for (int chunk = 0; chunk < D / kChunk; ++chunk) {
+    for (int c = 0; c < D / 16; ++c) {
+      Words x{};
+      if (valid && a.scale != 0) x = *reinterpret_cast<const Words*>(from + 16 * c + 8 * w.half) ^ flip;
+      w.q[c] = __builtin_bit_cast(Eight, x);
+    }
+  };
 #pragma unroll
-      for (int x = 0; x < kChunk / 32; ++x)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float4 y;
-          float* z = &y.x;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) z[r] = w.o[t][chunk * (kChunk / 32) + x][4 * j + r] * weight;
-          *reinterpret_cast<float4*>(&parts[wave][lane & 31][32 * x + 8 * j + 4 * w.half]) = y;
-        }
-      __syncthreads();
-      constexpr int kMine = kChunk / 8;
-      float y[8] = {};
-#pragma unroll
-      for (int x = 0; x < kRowWaves; ++x)
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) y[i] += parts[x][col][part * kMine + i];
-#pragma unroll
-      for (int i = 0; i < kMine; ++i) y[i] = sum == 0.0f ? 0.0f : y[i] * over;
-      if (token >= 0) {
-        const int64_t at = (DIRECT ? to : place) * D + chunk * kChunk + part * kMine;
-        if constexpr (!DIRECT) {
-#pragma unroll
-          for (int i = 0; i < kMine; i += 4) *reinterpret_cast<float4*>(a.part_o + at + i) = *reinterpret_cast<float4*>(&y[i]);
-        } else if constexpr (kMine == 8) {
-          store8<T>(a.out, at, y);
-        } else {
-#pragma unroll
-          for (int i = 0; i < kMine; ++i) static_cast<typename T::One*>(a.out)[at + i] = (typename T::One)y[i];
-        }
+  for (int d = 1; d < 32; d *= 2) {
+    const int32_t x = __shfl_xor(all, d), y = __shfl_xor(most, d);
+    all = x < all ? x : all;
+    most = y > most ? y : most;
+  }
+  all = __builtin_amdgcn_readfirstlane(all);
+  most = __builtin_amdgcn_readfirstlane(most);
+
+  // its tokens: a part of those that some row of the tile sees
+  Run run{};
+  auto part = [&](Segment* to, const Held& held, int64_t at, int32_t parts, int32_t which, int32_t seen_by_all, int32_t seen_by_any) {
+    const int32_t blocks = (seen_by_any + kBlock - 1) / kBlock, per = (blocks + parts - 1) / parts, from = which * per < blocks ? which * per : blocks;
+    const int32_t own = blocks - from < per ? blocks - from : per, whole = seen_by_all / kBlock - from;
+    to->first = from;
+    to->whole = whole < 0 ? 0 : whole < own ? whole : own;
+    to->edge = own - to->whole;
+    to->data = held.data + (at + from) * held.block_bytes;
+    to->scale = FP8 ? held.scale + (at + from) * kScaleBytes : nullptr;
+  };
+  if (prompt || a.how == kDirect) part(&run.prompt, a.prompt, a.prompt.first(p, head, a.Hk), prompt ? (int32_t)splits : 1, prompt ? split : 0, prompt_len, prompt_len);
+  if (!prompt)
+    part(&run.path, a.path, a.path.first(row, head, a.Hk), (int32_t)splits, split, clamped(path_len - count + first / a.G + 1, path_len),
+         clamped(path_len - count + (first + here - 1) / a.G + 1, path_len));
+  {
+    const uint8_t* own = ring + (solo ? wave : turn) * (R::kBytes / (solo ? kWaves : turns));
+    bool odd;
+    if (groups == 1) odd = stream<T, D, FP8, 1>(w, run, own, group, turn, turns, prompt_len, sees, all, most, queries);
+    else if (groups == 2) odd = stream<T, D, FP8, 2>(w, run, own, group, turn, turns, prompt_len, sees, all, most, queries);
+    else odd = stream<T, D, FP8, 4>(w, run, own, group, turn, turns, prompt_len, sees, all, most, queries);
+    if (odd) {                                           // (of a path: a prompt's tokens are seen by all or by none)
+      for (int32_t x = turn; x < run.blocks(); x += turns) {
+        bool path;
+        const int64_t at = run.place(x, &path);
+        const int32_t block = kBlock * ((int32_t)at + run.path.first);
+        if (path && at >= run.path.whole)
+          w.odd_values(run.path.data + at * a.path.block_bytes, FP8 ? run.path.scale + at * kScaleBytes : nullptr, sees - block, all - block, most - block);
       }
-      __syncthreads();
+    }
+  }
+
+  // the sums of the waves of the same rows joined, and each row's factor
+  auto sync = [&] {
+    if (solo) wave_sync();
+    else __syncthreads();
+  };
+  float sum = both_sum(w.l), top = w.m, factor = 1.0f;
+  if (turns > 1) {
+    if (lane < 32) {
+      tops[wave][lane] = top;
+      sums[wave][lane] = sum;
+    }
+    __syncthreads();
+    float high = kNone, whole = 0;
+    for (int x = 0; x < turns; ++x) high = fmaxf(high, tops[group + x * groups][lane & 31]);
+    for (int x = 0; x < turns; ++x) {
+      const float m = tops[group + x * groups][lane & 31];
+      whole += sums[group + x * groups][lane & 31] * (m == kNone ? (high == kNone ? 1.0f : 0.0f) : exp2_fast(m - high));
+    }
+    factor = top == kNone ? (high == kNone ? 1.0f : 0.0f) : exp2_fast(top - high);
+    sum = whole;
+    top = high;
+  }
+  factor = sum == 0.0f ? 0.0f : factor / sum;
+  const float lse = sum == 0.0f ? kNone : top + __builtin_amdgcn_logf(sum);            // base 2
+  const int64_t problem = (int64_t)p * a.N * a.n * a.H;  // the problem's first row
+  if (turn == 0 && lane < 32) {
+    places[solo ? wave : group][lane] = valid ? own_place : -1;
+    lses[solo ? wave : group][lane] = lse;
+    if (valid && !results) a.part_lse[(int64_t)(prompt ? split : a.prompt_splits + split) * a.rows + problem + own_place] = lse;
+    if (valid && a.how == kDirect && a.lse) a.lse[problem + own_place] = lse * 0.693147180559945309f;
+  }
+  // O: eight threads a row, kMine values each
+  auto part_of = [&](int32_t x) { return reinterpret_cast<Part*>(ring + x * (R::kBytes / kWaves)); };
+#pragma unroll
+  for (int chunk = 0; chunk < D / kChunk; ++chunk) {
+    sync();                                              // (the ring, or the last chunk, has been read)
+#pragma unroll
+    for (int x = 0; x < kChunk / 32; ++x)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float4 y;
+        float* z = &y.x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[r] = sum == 0.0f ? 0.0f : w.o[chunk * (kChunk / 32) + x][4 * j + r] * factor;
+        *reinterpret_cast<float4*>(&part_of(wave)[lane & 31][32 * x + 8 * j + 4 * w.half]) = y;
+      }
+    sync();
+    for (int32_t x = solo ? lane : threadIdx.x; x < groups * 256; x += solo ? 64 : 64 * kWaves) {
+      const int32_t c = solo ? wave : x / 256, col = x / 8 & 31, part = x & 7, place = places[c][col];
+      if (place < 0) continue;
+      float y[8] = {};
+      for (int s = 0; s < turns; ++s)
+#pragma unroll
+        for (int r = 0; r < kMine; ++r) y[r] += part_of(c + s * groups)[col][part * kMine + r];
+      const int64_t to = problem + place;
+      const int32_t d = chunk * kChunk + part * kMine;
+      if (!results) {
+        float* out = a.part_o + ((int64_t)(prompt ? split : a.prompt_splits + split) * a.rows + to) * D + d;
+#pragma unroll
+        for (int r = 0; r < kMine; r += 4) *reinterpret_cast<float4*>(out + r) = float4{y[r], y[r + 1], y[r + 2], y[r + 3]};
+        continue;
+      }
+      if (a.how == kFinal) {
+        const float own = lses[c][col];
+        float best = own;
+        for (int s = 0; s < a.prompt_splits; ++s) best = fmaxf(best, a.part_lse[s * a.rows + to]);
+        // (nothing seen anywhere: zeros; a NaN is one in the sum already)
+        float whole = own == kNone ? 0.0f : exp2_fast(own - best);
+#pragma unroll
+        for (int r = 0; r < kMine; ++r) y[r] *= whole;
+        for (int s = 0; s < a.prompt_splits; ++s) {
+          const float other = a.part_lse[s * a.rows + to];
+          if (other == kNone) continue;
+          const float share = exp2_fast(other - best);
+          whole += share;
+          const float* from = a.part_o + (s * a.rows + to) * D + d;
+#pragma unroll
+          for (int r = 0; r < kMine; ++r) y[r] += share * from[r];
+        }
+        const float over = whole == 0.0f ? 0.0f : 1.0f / whole;
+#pragma unroll
+        for (int r = 0; r < kMine; ++r) y[r] *= over;
+        if (a.lse && chunk == 0 && part == 0) a.lse[to] = whole == 0.0f ? kNone : (best + __builtin_amdgcn_logf(whole)) * 0.693147180559945309f;
+      }
+      if constexpr (kMine == 8) {
+        store8<T>(a.out, to * D + d, y);
+      } else {
+#pragma unroll
+        for (int r = 0; r < kMine; ++r) static_cast<One*>(a.out)[to * D + d + r] = (One)y[r];
+      }
     }
   }
 }
@@ -267,17 +502,29 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   const int32_t parts = token % a.n < count ? a.prompt_splits + a.path_splits : 0;
   const int d = threadIdx.x % kLanes * 8;
   float top = kNone, sum = 0, y[8] = {};
+#pragma unroll 8
   for (int x = 0; x < parts; ++x) top = fmaxf(top, a.part_lse[x * a.rows + row]);
-  for (int x = 0; x < parts; ++x) {
-    const float lse = a.part_lse[x * a.rows + row];
-    if (lse == kNone) continue;                          // (nothing seen there)
-    const float weight = exp2_fast(lse - top);
-    sum += weight;
-    const float4* from = reinterpret_cast<const float4*>(a.part_o + (x * a.rows + row) * D + d);
-    const float4 lo = from[0], hi = from[1];
-    const float z[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  constexpr int kAhead = 4;
+  for (int x0 = 0; x0 < parts; x0 += kAhead) {
+    float lse[kAhead];
+    float4 part[kAhead][2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] += weight * z[i];
+    for (int s = 0; s < kAhead; ++s) {
+      const int64_t at = (x0 + s < parts ? x0 + s : x0) * a.rows + row;
+      lse[s] = x0 + s < parts ? a.part_lse[at] : kNone;
+      const float4* from = reinterpret_cast<const float4*>(a.part_o + at * D + d);
+      part[s][0] = from[0];
+      part[s][1] = from[1];
+    }
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+      if (lse[s] == kNone) continue;                     // (nothing seen there)
+      const float weight = exp2_fast(lse[s] - top);
+      sum += weight;
+      const float z[8] = {part[s][0].x, part[s][0].y, part[s][0].z, part[s][0].w, part[s][1].x, part[s][1].y, part[s][1].z, part[s][1].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] += weight * z[i];
+    }
   }
   const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
@@ -288,10 +535,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 
 template <class T, int D, bool FP8>
 void attend_as(const AttendArgs& a, const AttendLaunch& how, hipStream_t st) {
-  auto* kernel = how.wide ? (how.direct ? attend_rows_kernel<T, D, FP8, 2, true> : attend_rows_kernel<T, D, FP8, 2, false>)
-                          : (how.direct ? attend_rows_kernel<T, D, FP8, 1, true> : attend_rows_kernel<T, D, FP8, 1, false>);
-  kernel<<<how.items, 64 * kRowWaves, 0, st>>>(a);
-  if (!how.direct) {
+  attend_rows_kernel<T, D, FP8><<<how.groups, 64 * kWaves, 0, st>>>(a);
+  if (how.join) {
     constexpr int kRows = 256 / (D / 8);
     attend_join_kernel<T, D><<<(uint32_t)((a.rows + kRows - 1) / kRows), 256, 0, st>>>(a);
   }

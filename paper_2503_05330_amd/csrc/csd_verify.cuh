@@ -94,7 +94,16 @@ struct AttendArgs {
   int64_t rows;                      // P N n H
   int32_t prompt_splits, path_splits;
   int32_t prompt_tiles, path_tiles;  // tiles of query rows of a (problem, kv head), of a (path, kv head)
+  int32_t prompt_groups;             // workgroups of the prompts' items, before those of the paths'
+  int32_t solo;                      // a path's item is one wave's instead of a workgroup's
+  int32_t prompt_turns, path_turns;  // whether items that have tokens in common go to one XCD
+  int32_t how;                       // one of these
 };
+
+// What the items of a launch do.
+constexpr int32_t kParts = 0;            // prompts' and paths': parts, for attend_join_kernel
+constexpr int32_t kDirect = 1;           // paths' alone, with the whole prompt each: results
+constexpr int32_t kFinal = 2;            // paths' alone: joined with the prompts' parts of an earlier launch, results
 
 // What a call of csd_cache_write or csd_cache_read hands to its kernel.
 struct MoveArgs {
@@ -108,8 +117,8 @@ struct MoveArgs {
 
 // The shape of a call of csd_attend; every head_dim's kernels have a source of their own.
 struct AttendLaunch {
-  uint32_t items;                    // workgroups of attend_rows_kernel
-  bool wide, direct, f16, fp8;       // wide: tiles of 64 query rows instead of 32
+  uint32_t groups;                   // workgroups of attend_rows_kernel
+  bool join, f16, fp8;
 };
 void attend_64(const AttendArgs& a, const AttendLaunch& how, hipStream_t st);
 void attend_96(const AttendArgs& a, const AttendLaunch& how, hipStream_t st);
