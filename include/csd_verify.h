@@ -89,7 +89,7 @@ int csd_cache_destroy(csd_cache* cache);
  *   d_start   [P][N] ([P]) int32  position of a row's first token; NULL = 0
  *   d_counts  [P][N] ([P]) int32  how many of the n tokens row r really takes (clamped to [0, n]); NULL = n
  * Token t goes to position start + t, whatever was there: a loop that rejected drafts writes over them.  Tokens whose position
- * is outside of [0, capacity) are dropped and raise CSD_STATUS_CAPACITY (csd_cache_status).  n * n_kv_heads <= 2^28. */
+ * is outside of [0, capacity) are dropped and raise CSD_STATUS_CAPACITY (csd_cache_status). */
 int csd_cache_write(csd_cache* cache, int32_t layer, const csd_heads* k, const csd_heads* v, const int32_t* d_start,
                     const int32_t* d_counts, int32_t n, void* stream);
 int csd_cache_write_prompt(csd_cache* cache, int32_t layer, const csd_heads* k, const csd_heads* v, const int32_t* d_start,

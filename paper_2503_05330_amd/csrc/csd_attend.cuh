@@ -43,7 +43,8 @@ struct Staged {
   static constexpr int kBytes = 2 * kHalf + (FP8 ? kScaleBytes : 0);
   const uint8_t* at;
   __device__ Words keys(int c, int lane) const { return *reinterpret_cast<const Words*>(at + c * 1024 + lane * 16); }
-  __device__ Words values(int c, int lane) const { return *reinterpret_cast<const Words*>(at + kHalf + c * 1024 + lane * 16); }
+  typedef typename std::conditional<FP8, Pair, Words>::type Values;    // eight tokens' of a d
+  __device__ Values values(int c, int lane) const { return reinterpret_cast<const Values*>(at + kHalf)[c * 64 + lane]; }
   __device__ const uint8_t* scales() const { return at + 2 * kHalf; }
 };
 
@@ -88,24 +89,29 @@ struct Wave {
     return s;
   }
 
-  // Scores to weights (times their values' scales), with the running maximum and sum.  EDGE: the row sees the block's first `sees`
-  // tokens.
-  template <bool EDGE>
-  __device__ void softmax(Acc& s, const Staged<D, FP8>& b, int32_t sees) {
-    uint32_t exps[4];                                    // of the lane's 16 tokens' values
+  // Scores of PER blocks to weights (times their values' scales), with the running maximum and sum.  EDGE: the row sees a block's first
+  // `sees` tokens.
+  template <bool EDGE, int PER>
+  __device__ void softmax(Acc (&s)[PER], const Staged<D, FP8> (&b)[PER], const int32_t (&sees)[PER]) {
+    uint32_t exps[PER][4];                               // of the lane's 16 tokens' values
     if constexpr (FP8) {
-      const Pair lo = *reinterpret_cast<const Pair*>(b.scales() + kBlock + 8 * half), hi = *reinterpret_cast<const Pair*>(b.scales() + kBlock + 16 + 8 * half);
-      exps[0] = lo[0], exps[1] = lo[1], exps[2] = hi[0], exps[3] = hi[1];
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        const Pair lo = *reinterpret_cast<const Pair*>(b[e].scales() + kBlock + 8 * half), hi = *reinterpret_cast<const Pair*>(b[e].scales() + kBlock + 16 + 8 * half);
+        exps[e][0] = lo[0], exps[e][1] = lo[1], exps[e][2] = hi[0], exps[e][3] = hi[1];
+      }
     }
-    auto exponent = [&](int r) { return exps[r / 4] >> 8 * (r & 3) & 0xff; };
+    auto exponent = [&](int e, int r) { return exps[e][r / 4] >> 8 * (r & 3) & 0xff; };
     constexpr bool kAdded = FP8 && is_half();
     float most = kNone;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      if constexpr (kAdded) s[r] = fmaf(s[r], scale, (float)exponent(r) - 127.0f);
-      if constexpr (EDGE) s[r] = token_of(r, half) < sees ? s[r] : kNone;
-      most = fmaxf(most, s[r]);
-    }
+    for (int e = 0; e < PER; ++e)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if constexpr (kAdded) s[e][r] = fmaf(s[e][r], scale, (float)exponent(e, r) - 127.0f);
+        if constexpr (EDGE) s[e][r] = token_of(r, half) < sees[e] ? s[e][r] : kNone;
+        most = fmaxf(most, s[e][r]);
+      }
     most = fmaxf(m, kAdded ? both_max(most) : both_max(most) * scale);
     if (__ballot(most > m)) {                            // (m -inf: nothing has been summed)
       const float down = m == kNone ? 0.0f : exp2_fast(m - most);
@@ -116,43 +122,48 @@ struct Wave {
     }
     const float base = m == kNone ? 0.0f : m;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = exp2_fast(kAdded ? s[r] - base : fmaf(s[r], scale, -base));
-      if constexpr (!FP8) {
-        l += s[r];
-      } else if constexpr (kAdded) {
-        const float up = __uint_as_float((254 - exponent(r)) << 23);
-        if constexpr (EDGE) l += token_of(r, half) < sees ? s[r] * up : 0.0f;
-        else l = fmaf(s[r], up, l);
-      } else {
-        l += s[r];
-        const float up = __uint_as_float(exponent(r) << 23);
-        if constexpr (EDGE) s[r] = token_of(r, half) < sees ? s[r] * up : 0.0f;
-        else s[r] *= up;
+    for (int e = 0; e < PER; ++e)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[e][r] = exp2_fast(kAdded ? s[e][r] - base : fmaf(s[e][r], scale, -base));
+        if constexpr (!FP8) {
+          l += s[e][r];
+        } else if constexpr (kAdded) {
+          const float up = __uint_as_float((254 - exponent(e, r)) << 23);
+          if constexpr (EDGE) l += token_of(r, half) < sees[e] ? s[e][r] * up : 0.0f;
+          else l = fmaf(s[e][r], up, l);
+        } else {
+          l += s[e][r];
+          const float up = __uint_as_float(exponent(e, r) << 23);
+          if constexpr (EDGE) s[e][r] = token_of(r, half) < sees[e] ? s[e][r] * up : 0.0f;
+          else s[e][r] *= up;
+        }
       }
-    }
   }
 
-  __device__ static Eight value_operand(Words w, int u) {
-    if constexpr (FP8) return from_fp8<T>(u ? Pair{w[2], w[3]} : Pair{w[0], w[1]}, 1.0f);
+  typedef typename Staged<D, FP8>::Values Values;
+  static constexpr int kWords = FP8 ? 2 : 4;
+  __device__ static Eight value_operand(Values w) {
+    if constexpr (FP8) return from_fp8<T>(w, 1.0f);
     else return __builtin_bit_cast(Eight, w);
   }
-  static constexpr int value_load(int x, int u) { return FP8 ? x : 2 * x + u; }
   // the bits of the first `to` tokens of the block in the operand of tokens 16 u ..
-  __device__ Words kept(int u, int to) const {
+  __device__ Values kept(int u, int to) const {
     const int n = to - 16 * u - 8 * half;                // of the operand's eight
     auto below = [](int bits) { return bits <= 0 ? 0ull : bits >= 64 ? ~0ull : (1ull << bits) - 1; };
-    Words w{};
-    const uint64_t low = below(n * (FP8 ? 8 : 16)), high = FP8 ? 0 : below(n * 16 - 64);
-    w[FP8 ? 2 * u : 0] = (uint32_t)low, w[FP8 ? 2 * u + 1 : 1] = (uint32_t)(low >> 32);
-    if constexpr (!FP8) w[2] = (uint32_t)high, w[3] = (uint32_t)(high >> 32);
+    Values w{};
+#pragma unroll
+    for (int i = 0; i < kWords; i += 2) {
+      const uint64_t bits = below(n * (FP8 ? 8 : 16) - 32 * i);
+      w[i] = (uint32_t)bits, w[i + 1] = (uint32_t)(bits >> 32);
+    }
     return w;
   }
   // all bits of the values that are an infinity or a NaN: whose exponent (8 bits: all but the sign) is all ones
-  __device__ static Words odd(Words w) {
+  __device__ static Values odd(Values w) {
     constexpr uint32_t kOnes = FP8 ? 0x7f7f7f7f : T::kExponent * 0x10001u, kLow = FP8 ? 0x01010101 : (T::kExponent & ~(T::kExponent << 1)) * 0x10001u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kWords; ++i) {
       const uint32_t top = ((w[i] & kOnes) + kLow) & (FP8 ? 0x80808080 : 0x80008000);
       w[i] = top | (top - (top >> (FP8 ? 7 : 15)));
     }
@@ -174,32 +185,28 @@ struct Wave {
     if constexpr (EDGE) {
       all = all < 0 ? 0 : all;
       if (all < most && all < kBlock) {
-        const Words sure[2] = {kept(0, all), kept(1, all)}, seen[2] = {kept(0, most), kept(1, most)};
+        const Values sure[2] = {kept(0, all), kept(1, all)}, seen[2] = {kept(0, most), kept(1, most)};
         uint32_t met = 0;
 #pragma unroll
-        for (int x = 0; x < kTiles; ++x) {
-          Words w{};
+        for (int x = 0; x < kTiles; ++x)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            if (u == 0 || !FP8) w = b.values(value_load(x, u), lane);
-            const Words strange = odd(w) & seen[u] & ~sure[u];
-            met |= strange[0] | strange[1] | strange[2] | strange[3];
-            o[x] = T::mfma(value_operand(w & seen[u] & ~strange, u), p[u], o[x]);
+            const Values w = b.values(2 * x + u, lane), strange = odd(w) & seen[u] & ~sure[u];
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) met |= strange[i];
+            o[x] = T::mfma(value_operand(w & seen[u] & ~strange), p[u], o[x]);
           }
-        }
         return met != 0;
       }
     }
-    const Words seen[2] = {kept(0, EDGE ? most : kBlock), kept(1, EDGE ? most : kBlock)};
+    const Values seen[2] = {kept(0, EDGE ? most : kBlock), kept(1, EDGE ? most : kBlock)};
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x) {
-      Words w{};
+    for (int x = 0; x < kTiles; ++x)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        if (u == 0 || !FP8) w = b.values(value_load(x, u), lane);
-        o[x] = T::mfma(value_operand(EDGE ? w & seen[u] : w, u), p[u], o[x]);
+        const Values w = b.values(2 * x + u, lane);
+        o[x] = T::mfma(value_operand(EDGE ? w & seen[u] : w), p[u], o[x]);
       }
-    }
     return false;
   }
   // What values() has left out of a block, which is read from memory again: one token after the other, for the rows that see it.
@@ -226,14 +233,14 @@ struct Wave {
     Eight p[2];
     weights(s, p);
     for (int32_t token = all < 0 ? 0 : all; token < most && token < kBlock; ++token) {
-      const Words alone[2] = {kept(0, token + 1) & ~kept(0, token), kept(1, token + 1) & ~kept(1, token)};
+      const Values alone[2] = {kept(0, token + 1) & ~kept(0, token), kept(1, token + 1) & ~kept(1, token)};
 #pragma unroll
       for (int x = 0; x < kTiles; ++x) {
         Acc one{};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const Words w = b.values(value_load(x, u), lane);
-          one = T::mfma(value_operand(w & odd(w) & alone[u], u), p[u], one);
+          const Values w = b.values(2 * x + u, lane);
+          one = T::mfma(value_operand(w & odd(w) & alone[u]), p[u], one);
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[x][r] += token < sees ? one[r] : 0.0f;

@@ -8,7 +8,7 @@
 //   of one path, and the run is a part of its own tokens (kDirect: the whole prompt, then the path), or
 //   of all paths of a problem, without gaps for tokens beyond the paths' counts, and the run is a part of the prompt.
 // Results are written at once where an item has seen all that its rows see, else as a part of each row, O / l and lse
-// in 32 bits, and attend_join_kernel (kFinal: the path's item) weighs the parts by 2^lse.
+// in 32 bits, and attend_join_kernel weighs the parts by 2^lse.
 #pragma once
 
 #include "csd_attend.cuh"
@@ -102,19 +102,26 @@ __device__ inline uint32_t lds_offset(const void* p) {
   return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p);
 }
 
-// The sizes of a ring: stages for two workgroups on a CU, where a stage for each wave leaves room for them.
+// The sizes of a ring: blocks for two workgroups on a CU where one for each wave leaves room for them.  (Twice the blocks, for launches of
+// no more workgroups than CUs, took 16 paths of 1024 + 1024 tokens from 20.4 to 22.1 us.)
 template <int D, bool FP8>
 struct Ring {
-  typedef Staged<D, FP8> Stage;
-  static constexpr int kKeys = Stage::kHalf / 1024;      // pieces of the keys, and of the values
-  static constexpr int stages() {
+  typedef Staged<D, FP8> Block;
+  static constexpr int kKeys = Block::kHalf / 1024;      // pieces of the keys, and of the values
+  static constexpr int blocks() {
     int x = kWaves;
-    while (x * 2 * Stage::kBytes <= 72 * 1024) x *= 2;
+    while (x * 2 * Block::kBytes <= 72 * 1024) x *= 2;
     return x;
   }
-  static constexpr int kStages = stages();
-  static constexpr int kBytes = kStages * Stage::kBytes;
+  static constexpr int kBlocks = blocks();
+  static constexpr int kBytes = kBlocks * Block::kBytes;
   static constexpr int kResident = kBytes <= 72 * 1024 && D <= 128 ? 2 : 1;   // workgroups of a CU
+  // Where C waves share blocks: how many blocks a round takes, and stages of so many.  (Two where that leaves two stages: an exchange of
+  // maxima and two barriers for 64 tokens.  64 paths x 17 tokens of 4096 + 4096: 132 us with one, 122 with two.)
+  template <int C>
+  static constexpr int round() { return kBlocks * C / kWaves >= 4 ? 2 : 1; }
+  template <int C>
+  static constexpr int stages() { return kBlocks * C / kWaves / round<C>(); }
   // loads of a wave when C waves share them
   template <int C>
   static constexpr int pieces() { return (kKeys + C - 1) / C; }
@@ -125,12 +132,12 @@ struct Ring {
     constexpr int N = pieces<C>();
     const uint32_t first = 1024u * (group * N < kKeys - N ? group * N : kKeys - N);
     fetch<N>(uniform(lds + first), uniform(block + first), lane * 16);
-    if constexpr (FP8) fetch_scales(uniform(lds + 2 * Stage::kHalf), uniform(scale), lane);
+    if constexpr (FP8) fetch_scales(uniform(lds + 2 * Block::kHalf), uniform(scale), lane);
   }
   template <int C>
   static __device__ void values(uint32_t lds, const uint8_t* block, int group, int lane) {
     constexpr int N = pieces<C>();
-    const uint32_t first = Stage::kHalf + 1024u * (group * N < kKeys - N ? group * N : kKeys - N);
+    const uint32_t first = Block::kHalf + 1024u * (group * N < kKeys - N ? group * N : kKeys - N);
     fetch<N>(uniform(lds + first), uniform(block + first), lane * 16);
   }
 };
@@ -156,34 +163,44 @@ struct Run {
   }
 };
 
-// Goes through the run's blocks turn, turn + turns, ..; C waves have the same blocks, the wave is the `group`th, and their share of the
-// ring is at `ring`.  prompt_len, sees: tokens of the prompt, of the path that the lane's row sees; all, most: of the path,
-// that all of the wave's rows, that any of them sees.  queries() loads the wave's queries, while the first blocks are on their way.
-// Returns whether there are values left for odd_values().
+// Goes through the run's blocks, kRound at a time: rounds turn, turn + turns, .. of them; C waves have the same blocks, the wave is the
+// `group`th, and their share of the ring is at `ring`.  prompt_len, sees: tokens of the prompt, of the path that the lane's row
+// sees; all, most: of the path, that all of the wave's rows, that any of them sees.  queries() loads the wave's queries, while
+// the first blocks are on their way.  Returns whether there are values left for odd_values().
 template <class T, int D, bool FP8, int C, class Queries>
 __device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, const uint8_t* ring, int32_t group, int32_t turn, int32_t turns,
                               int32_t prompt_len, int32_t sees, int32_t all, int32_t most, Queries queries) {
   typedef Ring<D, FP8> R;
-  constexpr int64_t kBlockBytes = 2 * R::Stage::kHalf;
+  typedef typename R::Block Block;
+  constexpr int64_t kBlockBytes = 2 * Block::kHalf;
   constexpr bool kShared = C > 1;
-  constexpr int kStages = R::kStages / kWaves * C;
+  constexpr int kRound = R::template round<C>(), kStages = R::template stages<C>();
   const uint32_t lds = uniform(lds_offset(ring));
-  const int32_t whole = run.whole(), blocks = run.blocks();
-  const int32_t mine = blocks > turn ? (blocks - turn + turns - 1) / turns : 0;
-  const int32_t rounds = kShared ? (blocks + turns - 1) / turns : mine;       // (all waves meet equally often)
+  const int32_t blocks = run.blocks(), in_all = (blocks + kRound - 1) / kRound;
+  const int32_t mine = in_all > turn ? (in_all - turn + turns - 1) / turns : 0;
+  const int32_t rounds = kShared ? (in_all + turns - 1) / turns : mine;       // (all waves meet equally often)
+  const int32_t whole = run.whole() / kRound;            // rounds of blocks that all rows see whole
   auto load_keys = [&](int32_t j, int32_t stage) {
-    bool path;
-    const int64_t at = run.place(turn + j * turns, &path);
-    R::template keys<C>(lds + stage * R::Stage::kBytes, (path ? run.path.data : run.prompt.data) + at * kBlockBytes,
-                        (path ? run.path.scale : run.prompt.scale) + (FP8 ? at * kScaleBytes : 0), group, w.lane);
+#pragma unroll
+    for (int e = 0; e < kRound; ++e) {
+      const int32_t x = (turn + j * turns) * kRound + e;
+      bool path;
+      const int64_t at = run.place(x < blocks ? x : blocks - 1, &path);       // (the same number of loads in every round)
+      R::template keys<C>(lds + (stage * kRound + e) * Block::kBytes, (path ? run.path.data : run.prompt.data) + at * kBlockBytes,
+                          (path ? run.path.scale : run.prompt.scale) + (FP8 ? at * kScaleBytes : 0), group, w.lane);
+    }
   };
   auto load_values = [&](int32_t j, int32_t stage) {
-    bool path;
-    const int64_t at = run.place(turn + j * turns, &path);
-    R::template values<C>(lds + stage * R::Stage::kBytes, (path ? run.path.data : run.prompt.data) + at * kBlockBytes, group, w.lane);
+#pragma unroll
+    for (int e = 0; e < kRound; ++e) {
+      const int32_t x = (turn + j * turns) * kRound + e;
+      bool path;
+      const int64_t at = run.place(x < blocks ? x : blocks - 1, &path);
+      R::template values<C>(lds + (stage * kRound + e) * Block::kBytes, (path ? run.path.data : run.prompt.data) + at * kBlockBytes, group, w.lane);
+    }
   };
-  // until the loads before the newest (kStages - 1) * kLoads + MORE are done, if so many have been issued behind them
-  constexpr int kKeyLoads = R::template pieces<C>() + (FP8 ? 1 : 0), kValueLoads = R::template pieces<C>();
+  // until the loads before the newest (kStages - 1) rounds' and MORE are done, if so many have been issued behind them
+  constexpr int kKeyLoads = kRound * (R::template pieces<C>() + (FP8 ? 1 : 0)), kValueLoads = kRound * R::template pieces<C>();
   constexpr int kBehind = (kStages - 1) * (kKeyLoads + kValueLoads);
   auto wait = [&](bool behind, auto more) {
     if (behind) wait_loads<kBehind + decltype(more)::value>();
@@ -201,22 +218,32 @@ __device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, const uint8_t*
   auto round = [&](int32_t j, auto edge_of) {
     constexpr bool kEdge = decltype(edge_of)::value;
     const bool here = j < mine;
-    const typename R::Stage b{ring + stage * R::Stage::kBytes};
-    bool path = false;
-    int32_t first = 0;
-    if constexpr (kEdge) {
-      const int32_t at = run.place(turn + j * turns, &path);
-      first = kBlock * (at + (path ? run.path.first : run.prompt.first));
+    Block b[kRound];
+    int32_t seen[kRound] = {}, seen_all[kRound] = {}, seen_any[kRound] = {};
+#pragma unroll
+    for (int e = 0; e < kRound; ++e) {
+      b[e].at = ring + (stage * kRound + e) * Block::kBytes;
+      if constexpr (kEdge) {
+        const int32_t x = (turn + j * turns) * kRound + e;
+        bool path = false;
+        if (x < blocks) {
+          const int32_t at = run.place(x, &path), first = kBlock * (at + (path ? run.path.first : run.prompt.first));
+          seen[e] = (path ? sees : prompt_len) - first;
+          seen_all[e] = (path ? all : prompt_len) - first;
+          seen_any[e] = (path ? most : prompt_len) - first;
+        }
+      }
     }
-    Acc s;
+    Acc s[kRound];
     wait(j + kStages - 1 < mine, std::integral_constant<int, kShared ? 0 : kValueLoads>{});
     if constexpr (kShared) {
-      meet();                                            // the keys are there, and all are done with the last block's values
+      meet();                                            // the keys are there, and all are done with the last round's values
       if (j + kStages - 1 < mine) load_values(j + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
     }
     if (here) {
-      s = w.scores(b);
-      w.template softmax<kEdge>(s, b, (path ? sees : prompt_len) - first);
+#pragma unroll
+      for (int e = 0; e < kRound; ++e) s[e] = w.scores(b[e]);
+      w.template softmax<kEdge, kRound>(s, b, seen);
     }
     if constexpr (kShared) {
       wait(j + kStages - 1 < mine, std::integral_constant<int, 0>{});
@@ -227,7 +254,10 @@ __device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, const uint8_t*
       if (j + kStages < mine) load_keys(j + kStages, stage);
       wait(j + kStages < mine, std::integral_constant<int, kKeyLoads>{});
     }
-    if (here) met |= w.template values<kEdge>(s, b, (path ? all : prompt_len) - first, (path ? most : prompt_len) - first);
+    if (here) {
+#pragma unroll
+      for (int e = 0; e < kRound; ++e) met |= w.template values<kEdge>(s[e], b[e], seen_all[e], seen_any[e]);
+    }
     if constexpr (!kShared) {
       if (j + kStages < mine) load_values(j + kStages, stage);
     }
@@ -255,14 +285,14 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
   static_assert(sizeof(Part) * 32 <= R::kBytes / kWaves && R::kBytes / kWaves % 16 == 0);
   __shared__ Slots slots;
   __shared__ int32_t packed;
-  __shared__ float tops[kWaves][32], sums[kWaves][32], lses[kWaves][32];
+  __shared__ float tops[kWaves][32], sums[kWaves][32];
   __shared__ int32_t places[kWaves][32];
   __shared__ alignas(16) uint8_t ring[R::kBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // the item
   const bool prompt = (int32_t)blockIdx.x < a.prompt_groups;
-  const bool solo = !prompt && a.solo, results = !prompt && a.how != kParts;
+  const bool solo = !prompt && a.solo, results = a.how == kDirect;
   uint32_t item = blockIdx.x;
   if (!prompt) item -= a.prompt_groups;
   if (solo) item = item * kWaves + wave;
@@ -387,11 +417,12 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
     else if (groups == 2) odd = stream<T, D, FP8, 2>(w, run, own, group, turn, turns, prompt_len, sees, all, most, queries);
     else odd = stream<T, D, FP8, 4>(w, run, own, group, turn, turns, prompt_len, sees, all, most, queries);
     if (odd) {                                           // (of a path: a prompt's tokens are seen by all or by none)
-      for (int32_t x = turn; x < run.blocks(); x += turns) {
+      const int32_t round = groups == 1 ? R::template round<1>() : groups == 2 ? R::template round<2>() : R::template round<4>();
+      for (int32_t x = run.whole() / round * round; x < run.blocks(); ++x) {
         bool path;
         const int64_t at = run.place(x, &path);
         const int32_t block = kBlock * ((int32_t)at + run.path.first);
-        if (path && at >= run.path.whole)
+        if (path && x / round % turns == turn)
           w.odd_values(run.path.data + at * a.path.block_bytes, FP8 ? run.path.scale + at * kScaleBytes : nullptr, sees - block, all - block, most - block);
       }
     }
@@ -424,9 +455,8 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
   const int64_t problem = (int64_t)p * a.N * a.n * a.H;  // the problem's first row
   if (turn == 0 && lane < 32) {
     places[solo ? wave : group][lane] = valid ? own_place : -1;
-    lses[solo ? wave : group][lane] = lse;
     if (valid && !results) a.part_lse[(int64_t)(prompt ? split : a.prompt_splits + split) * a.rows + problem + own_place] = lse;
-    if (valid && a.how == kDirect && a.lse) a.lse[problem + own_place] = lse * 0.693147180559945309f;
+    if (valid && results && a.lse) a.lse[problem + own_place] = lse * 0.693147180559945309f;
   }
   // O: eight threads a row, kMine values each
   auto part_of = [&](int32_t x) { return reinterpret_cast<Part*>(ring + x * (R::kBytes / kWaves)); };
@@ -458,28 +488,6 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
 #pragma unroll
         for (int r = 0; r < kMine; r += 4) *reinterpret_cast<float4*>(out + r) = float4{y[r], y[r + 1], y[r + 2], y[r + 3]};
         continue;
-      }
-      if (a.how == kFinal) {
-        const float own = lses[c][col];
-        float best = own;
-        for (int s = 0; s < a.prompt_splits; ++s) best = fmaxf(best, a.part_lse[s * a.rows + to]);
-        // (nothing seen anywhere: zeros; a NaN is one in the sum already)
-        float whole = own == kNone ? 0.0f : exp2_fast(own - best);
-#pragma unroll
-        for (int r = 0; r < kMine; ++r) y[r] *= whole;
-        for (int s = 0; s < a.prompt_splits; ++s) {
-          const float other = a.part_lse[s * a.rows + to];
-          if (other == kNone) continue;
-          const float share = exp2_fast(other - best);
-          whole += share;
-          const float* from = a.part_o + (s * a.rows + to) * D + d;
-#pragma unroll
-          for (int r = 0; r < kMine; ++r) y[r] += share * from[r];
-        }
-        const float over = whole == 0.0f ? 0.0f : 1.0f / whole;
-#pragma unroll
-        for (int r = 0; r < kMine; ++r) y[r] *= over;
-        if (a.lse && chunk == 0 && part == 0) a.lse[to] = whole == 0.0f ? kNone : (best + __builtin_amdgcn_logf(whole)) * 0.693147180559945309f;
       }
       if constexpr (kMine == 8) {
         store8<T>(a.out, to * D + d, y);

@@ -3,11 +3,11 @@
 // Layout.  Attention multiplies tiles of 32 tokens on the matrix cores: scores S^T = K Q^T (rows: tokens, columns: query
 // rows), then O^T += V^T P^T, both by v_mfma_f32_32x32x16, whose operands are 8 consecutive values of the contracted
 // axis per lane.  The cache holds blocks of 32 tokens of one head in the order in which a wave's lanes take these
-// operands, 16 bytes a lane, so that a load is 1 KB without gaps and goes to registers (or linearly to LDS) as it is:
+// operands, so that a copy to LDS is linear and the reads from there are without gaps (eight tokens' values lie together, so a
+// token that is written alone touches the lines of seven others, not those of all 32):
 //   keys    16-bit  [D/16][half][row m][8 d's]          d = 16 c + 8 half + i
 //           8-bit   [D/32][half][row m][2][8 d's]       two operands in a lane's 16 bytes
-//   values  16-bit  [D/32][2][half][32 d's][8 tokens]   token = 16 u + 8 half + i
-//           8-bit   [D/32][half][32 d's][2][8 tokens]
+//   values  either  [D/32][2][half][32 d's][8 tokens]   token = 16 u + 8 half + i
 // The result S^T leaves tokens 8 j + 4 half + r of its 32 rows in register 4 j + r of a lane.  With keys in row
 // m(token) = the token's bits 2 and 3 exchanged, the lane's registers 8 u .. 8 u + 7 are tokens 16 u + 8 half ..
 // + 7: the operand P^T of the second product without moving anything between lanes.
@@ -103,7 +103,6 @@ struct AttendArgs {
 // What the items of a launch do.
 constexpr int32_t kParts = 0;            // prompts' and paths': parts, for attend_join_kernel
 constexpr int32_t kDirect = 1;           // paths' alone, with the whole prompt each: results
-constexpr int32_t kFinal = 2;            // paths' alone: joined with the prompts' parts of an earlier launch, results
 
 // What a call of csd_cache_write or csd_cache_read hands to its kernel.
 struct MoveArgs {

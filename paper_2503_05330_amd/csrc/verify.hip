@@ -123,8 +123,7 @@ int move(csd_cache* c, bool read, bool prompt, int32_t layer, const csd_heads& k
 }
 
 int check_move(const csd_cache* c, int32_t layer, int32_t n) {
-  if (!c || layer < 0 || layer >= c->cfg.n_layers || n <= 0 || n > CSD_MAX_CACHE_TOKENS || (int64_t)n * c->cfg.n_kv_heads > (1 << 28))
-    return CSD_ERR_INVALID_ARG;
+  if (!c || layer < 0 || layer >= c->cfg.n_layers || n <= 0 || n > CSD_MAX_CACHE_TOKENS) return CSD_ERR_INVALID_ARG;
   return CSD_OK;
 }
 int write(csd_cache* c, bool prompt, int32_t layer, const csd_heads* k, const csd_heads* v, const int32_t* start, const int32_t* counts,

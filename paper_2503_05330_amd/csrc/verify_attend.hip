@@ -19,19 +19,53 @@ void attend_dim(const AttendArgs& a, const AttendLaunch& how, int32_t head_dim, 
 struct Shape {
   int32_t how;
   bool solo;
-  int64_t groups, least;   // workgroups that an axis is split for, and the fewest blocks of a part
+  int64_t prompt_tiles, path_tiles, prompt_splits, path_splits;
 };
 
-// rows: query rows of a path and kv head
-Shape shape_of(int64_t problems, int64_t N, int64_t rows, int64_t prompt_blocks, int64_t path_blocks) {
-  const int64_t items = problems * N * over(rows, 32 * 4);
-  // products of 32 x 32: with the whole prompt for each path, with the prompt once for all rows of a problem
-  const int64_t direct = problems * N * over(rows, 32) * (prompt_blocks + path_blocks);
-  const int64_t shared = problems * over(N * rows, 32) * prompt_blocks + problems * N * over(rows, 32) * path_blocks;
-  const int64_t rounds = (prompt_blocks + path_blocks) * over(rows, 32) / 4;
-  if (prompt_blocks == 0 && items >= 512) return Shape{kDirect, rows <= 32 && items >= 2048, 0, 0};
-  if (rounds <= 16 || (items >= 2048 && 2 * direct <= 3 * shared)) return Shape{kDirect, false, 0, 0};
-  return Shape{kParts, rows <= 32 && items >= 2048, 512, 8};
+// The forms of a launch, and what each takes, ns, as far as the sizes tell: a start, the blocks that a wave goes through one after
+// the other, all blocks and all workgroups over what the chip holds of them (two workgroups a CU), and the parts that are written
+// and read again.  Fits of the measured times of 460 draws of 1 .. 64 problems of 1 .. 64 paths, 1 .. 17 tokens, prompts of 1 .. 8192
+// and paths of 2 .. 4100 tokens, heads of 64 and 128; each fit misses by 18 .. 20 %.  The form with the smallest is 2.6 % slower than
+// the fastest of 13 (parts split for 256, 512 or 1024 workgroups and 4, 8 or 16 blocks at least; geometric mean, 1.37
+// times at worst).  The best of one form for all sizes is 22 % slower: one launch with the whole prompt for each path.
+struct Cost {
+  int64_t start, round, blocks, groups, parts;
+  int64_t operator()(double rounds, double all_blocks, double all_groups, double part_values) const {
+    return start + (int64_t)(round * rounds + blocks * (all_blocks / kHeld) + groups * (all_groups / kHeld) + parts * (part_values / 1e6));
+  }
+  static constexpr double kHeld = 512;
+};
+
+Shape shape_of(int64_t problems, int64_t N, int64_t rows, int64_t head_dim, int64_t prompt_blocks, int64_t path_blocks) {
+  const int64_t paths = problems * N, both = prompt_blocks + path_blocks;
+  auto groups_of = [](int64_t x) { return x <= 32 ? 1 : x <= 64 ? 2 : 4; };             // of 32 rows in a tile of 128
+  const int64_t tiles = over(rows, 128), solo_tiles = over(rows, 32);
+  const double share = groups_of(rows) / 4.0;                                            // of a workgroup that has a block
+  Shape best{kDirect, false, 0, tiles, 0, 1};
+  int64_t least = Cost{8400, 470, 800, 4900, 0}(both * share, (double)paths * tiles * both * share, (double)paths * tiles, 0);
+  auto offer = [&](const Shape& s, int64_t cost) {
+    if (cost < least) best = s, least = cost;
+  };
+  // a wave an item
+  offer(Shape{kDirect, true, 0, solo_tiles, 0, 1},
+        Cost{8300, 530, 840, 6300, 0}(both, (double)paths * solo_tiles * both / 4, (double)paths * solo_tiles / 4, 0));
+  // the prompt's part for all paths together
+  for (const bool solo : {false, true}) {
+    const int64_t path_tiles = solo ? solo_tiles : tiles, prompt_tiles = over(N * rows, 128);
+    auto splits = [&](int64_t blocks, int64_t items) {
+      const int64_t most = over(blocks, solo ? 8 : 16), x = over(512, items);
+      return x < most ? x : most;
+    };
+    const int64_t s = prompt_blocks ? splits(prompt_blocks, problems * prompt_tiles) : 0, t = splits(path_blocks, paths * path_tiles);
+    const double prompt_share = groups_of(N * rows) / 4.0, path_share = solo ? 0.25 : share;
+    const double prompt_rounds = s ? over(prompt_blocks, s) * prompt_share : 0, path_rounds = over(path_blocks, t) * (solo ? 1 : share);
+    const double all = (double)problems * prompt_tiles * prompt_blocks * prompt_share + (double)paths * path_tiles * path_blocks * path_share;
+    const double groups = (double)problems * prompt_tiles * s + (double)paths * path_tiles * t / (solo ? 4 : 1);
+    const double values = (double)paths * rows * (s + t) * head_dim;
+    const Cost cost = solo ? Cost{11400, 590, 640, 6700, 860} : Cost{11600, 410, 650, 7200, 420};
+    offer(Shape{kParts, solo, prompt_tiles, path_tiles, s, t}, cost(prompt_rounds > path_rounds ? prompt_rounds : path_rounds, all, groups, values));
+  }
+  return best;
 }
 
 }  // namespace
@@ -39,19 +73,13 @@ Shape shape_of(int64_t problems, int64_t N, int64_t rows, int64_t prompt_blocks,
 void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound, int32_t path_bound, int64_t parts, hipStream_t st) {
   const int64_t prompt_blocks = over(prompt_bound, kBlock), path_blocks = over(path_bound, kBlock);
   const int64_t paths = (int64_t)a.P * a.N * a.Hk, problems = (int64_t)a.P * a.Hk;
-  const Shape shape = shape_of(problems, a.N, a.n * a.G, prompt_blocks, path_blocks);
+  const Shape shape = shape_of(problems, a.N, a.n * a.G, cfg.head_dim, prompt_blocks, path_blocks);
   a.how = shape.how;
   a.solo = shape.solo;
-  a.path_tiles = (int32_t)over(a.n * a.G, shape.solo ? 32 : 128);
-  a.prompt_tiles = (int32_t)over((int64_t)a.N * a.n * a.G, 128);
-  a.prompt_splits = a.how == kDirect || prompt_blocks == 0 ? 0 : 1;
-  a.path_splits = 1;
-  auto splits = [&](int64_t blocks, int64_t tiles) {
-    const int64_t most = over(blocks, shape.least), x = over(shape.groups, tiles);
-    return (int32_t)(x < most ? x : most);
-  };
-  if (a.prompt_splits) a.prompt_splits = splits(prompt_blocks, problems * a.prompt_tiles);
-  if (a.how == kParts) a.path_splits = splits(path_blocks, paths * a.path_tiles);
+  a.prompt_tiles = (int32_t)shape.prompt_tiles;
+  a.path_tiles = (int32_t)shape.path_tiles;
+  a.prompt_splits = (int32_t)shape.prompt_splits;
+  a.path_splits = (int32_t)shape.path_splits;
   while ((int64_t)(a.prompt_splits + a.path_splits) * a.rows > parts) {
     if (a.prompt_splits > a.path_splits) --a.prompt_splits;
     else --a.path_splits;
@@ -61,17 +89,9 @@ void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound,
   a.path_turns = a.how == kDirect && !a.solo && (problems % 8 == 0 || problems >= 64);
   const int64_t prompt_groups = a.prompt_turns ? over(chunks, 8) * 8 * a.prompt_tiles : chunks * a.prompt_tiles;
   const int64_t path_items = a.path_turns ? over(problems, 8) * 8 * a.N * a.path_tiles : paths * a.path_tiles * a.path_splits;
-  AttendLaunch how{0, false, cfg.type == CSD_F16, cfg.fp8 != 0};
-  if (a.how == kFinal && prompt_groups) {
-    AttendArgs b = a;
-    b.prompt_groups = (int32_t)prompt_groups;
-    b.how = kParts;
-    how.groups = (uint32_t)prompt_groups;
-    attend_dim(b, how, cfg.head_dim, st);
-  }
+  AttendLaunch how{0, a.how == kParts, cfg.type == CSD_F16, cfg.fp8 != 0};
   a.prompt_groups = a.how == kParts ? (int32_t)prompt_groups : 0;
   how.groups = (uint32_t)(a.prompt_groups + (a.solo ? over(path_items, 4) : path_items));
-  how.join = a.how == kParts;
   attend_dim(a, how, cfg.head_dim, st);
 }
 

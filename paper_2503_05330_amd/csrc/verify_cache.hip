@@ -1,44 +1,61 @@
 // csd — keys and values written to the cache of a verifying pass, and read back.
 //
-// A wave takes eight consecutive cache positions, aligned to eight, of one row and kv head: eight lanes a token, 16 bytes
-// each at a time, so that a token's largest value is found in three exchanges.  Keys go from these registers to their
-// place (pieces of eight d's stay together); values, which lie eight tokens together, are turned in LDS.  Where all eight
-// positions are written a value store is 16 (8-bit: 8) bytes, else the written tokens' elements alone: nothing is read
-// back, and no two waves write the same byte.  Waves next to each other take the heads of the same tokens, which lie
-// side by side in a projection's output.
+// A workgroup takes eight consecutive cache positions, aligned to eight, of one row; its waves take the kv heads, which lie
+// side by side in a projection's output, two at a time so that twice as much is on its way.  Eight lanes
+// hold a token, 16 bytes each at a time, so that a token's largest value is found in three exchanges.  Keys go from these
+// registers to their place (pieces of eight d's stay together); values, which lie eight tokens together, are turned in the
+// wave's part of LDS.  A value store is 16 (8-bit: 8) bytes: eight positions of a row and head are one wave's, so where not all of
+// them are written the others are read first and written back.
 #include "csd_verify.cuh"
 
 namespace csd {
 namespace verify {
 namespace {
 
-constexpr int kGroup = 8;               // positions of a wave
-constexpr int kMoveWaves = 4;
+constexpr int kGroup = 8;               // positions of a workgroup
+constexpr int kMoveWaves = 4, kHeads = 2;
 
 template <class T, bool FP8>
 struct Cell {
   typedef uint16_t Type;
+  typedef Words Eight;                  // a d's values of eight tokens
 };
 template <class T>
 struct Cell<T, true> {
   typedef uint8_t Type;
+  typedef Pair Eight;
 };
 
-// Where a wave's positions are.
+// Where a workgroup's positions are.
 struct Place {
   int64_t row, start, base;             // base: its first position
-  int32_t head, count;
-  __device__ Place(const MoveArgs& a, uint32_t wave) {
-    head = wave % a.Hk;
-    const uint32_t rest = wave / a.Hk;
-    row = rest / (uint32_t)a.groups;
-    const int32_t group = rest % (uint32_t)a.groups;
+  int32_t count;
+  __device__ Place(const MoveArgs& a) {
+    row = blockIdx.x / (uint32_t)a.groups;
+    const int32_t group = blockIdx.x % (uint32_t)a.groups;
     start = a.start ? a.start[row] : 0;
     count = a.counts ? a.counts[row] : a.n;
     count = count < 0 ? 0 : count > a.n ? a.n : count;
     base = (start & ~(int64_t)(kGroup - 1)) + kGroup * group;
   }
 };
+
+// Makes what the lanes of a wave have written to LDS visible to each other.
+__device__ inline void turn_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Where the values of eight tokens of a d lie in a block's values.
+template <bool FP8>
+__device__ inline int value_place(int d, int u, int half) {
+  return (((d / 32 * 2 + u) * 2 + half) * 32 + (d & 31)) * (FP8 ? 8 : 16);
+}
+// ... and eight d's of a token's keys in a block's keys.
+template <bool FP8>
+__device__ inline int key_place(int piece, int token) {
+  return FP8 ? (((piece >> 2) * 2 + (piece & 1)) * kBlock + key_row(token)) * 16 + (piece >> 1 & 1) * 8 : (piece * kBlock + key_row(token)) * 16;
+}
 
 // The exponent (biased) of the least power of two s with a <= 448 s = 1.75 * 2^8 s.
 __device__ inline uint32_t scale_exponent(float a) {
@@ -80,91 +97,99 @@ template <class T, int D, bool FP8>
 __global__ __launch_bounds__(64 * kMoveWaves) void cache_write_kernel(MoveArgs a) {
   typedef typename T::Eight Eight;
   typedef typename Cell<T, FP8>::Type One;
-  constexpr int kPieces = (D / 8 + 7) / 8;               // 16-byte pieces of a lane
+  typedef typename Cell<T, FP8>::Eight Tokens;
+  constexpr int kPieces = (D / 8 + 7) / 8, kColumns = (D + 63) / 64;   // of a lane: 16-byte pieces of a token, d's of eight tokens
   // (rows of D + 16 bytes apart: eight tokens' pieces in different banks, pieces aligned)
   __shared__ alignas(16) One turned[kMoveWaves][kGroup][D + 16 / sizeof(One)];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t number = blockIdx.x * kMoveWaves + wave;
-  const bool inside = number < (uint32_t)a.rows * a.groups * a.Hk;
-  const Place at(a, inside ? number : 0);
+  const Place at(a);
   const int64_t pos = at.base + (lane >> 3), t = pos - at.start;
-  const bool asked = inside && t >= 0 && t < at.count;
-  const bool live = asked && pos >= 0 && pos < a.held.cap;
-  if (asked && !live) atomicOr(a.status, CSD_STATUS_CAPACITY);
+  const bool asked = t >= 0 && t < at.count, live = asked && pos >= 0 && pos < a.held.cap;
+  if (wave == 0 && asked && !live) atomicOr(a.status, CSD_STATUS_CAPACITY);
   const uint64_t lives = __ballot(live);                 // eight lanes a token
-  Eight k[kPieces], v[kPieces];
-#pragma unroll
-  for (int x = 0; x < kPieces; ++x) {
-    const int d = ((lane & 7) + 8 * x) * 8;
-    k[x] = v[x] = Eight{};
-    if (live && d < D) {
-      k[x] = *reinterpret_cast<const Eight*>(static_cast<const typename T::One*>(a.k.data) + at.row * a.k.row_stride + t * a.k.token_stride + at.head * a.k.head_stride + d);
-      v[x] = *reinterpret_cast<const Eight*>(static_cast<const typename T::One*>(a.v.data) + at.row * a.v.row_stride + t * a.v.token_stride + at.head * a.v.head_stride + d);
-    }
-  }
-  const int64_t block = live ? a.held.first(at.row, at.head, a.Hk) + pos / kBlock : 0;
-  const int in_block = (int)(pos & (kBlock - 1));
-  uint8_t* const data = a.held.data + block * a.held.block_bytes;
-  float k_down = 1.0f, v_down = 1.0f;
-  if constexpr (FP8) {
-    float k_most = 0, v_most = 0;
-#pragma unroll
-    for (int x = 0; x < kPieces; ++x) {
-      k_most = largest<T>(k[x], k_most);
-      v_most = largest<T>(v[x], v_most);
-    }
-#pragma unroll
-    for (int r = 1; r < 8; r *= 2) {
-      k_most = fmaxf(k_most, __shfl_xor(k_most, r));
-      v_most = fmaxf(v_most, __shfl_xor(v_most, r));
-    }
-    const uint32_t k_exp = scale_exponent(k_most), v_exp = scale_exponent(v_most);
-    k_down = __uint_as_float((254 - k_exp) << 23);
-    v_down = __uint_as_float((254 - v_exp) << 23);
-    if (live && (lane & 7) == 0) {
-      uint8_t* const scale = a.held.scale + block * kScaleBytes;
-      scale[key_row(in_block)] = (uint8_t)k_exp;
-      scale[kBlock + in_block] = (uint8_t)v_exp;
-    }
-  }
-#pragma unroll
-  for (int x = 0; x < kPieces; ++x) {
-    const int piece = (lane & 7) + 8 * x;
-    if (piece * 8 >= D) continue;
-    if constexpr (FP8) {
-      const Pair codes = to_fp8<T>(k[x], k_down);
-      if (live)
-        *reinterpret_cast<Pair*>(data + (((piece >> 2) * 2 + (piece & 1)) * kBlock + key_row(in_block)) * 16 + (piece >> 1 & 1) * 8) = codes;
-      *reinterpret_cast<Pair*>(&turned[wave][lane >> 3][piece * 8]) = to_fp8<T>(v[x], v_down);
-    } else {
-      if (live) *reinterpret_cast<Eight*>(data + (piece * kBlock + key_row(in_block)) * 16) = k[x];
-      *reinterpret_cast<Eight*>(&turned[wave][lane >> 3][piece * 8]) = v[x];
-    }
-  }
-  __syncthreads();
   if (lives == 0) return;
-  // the wave's block, and its eight positions there
-  const int64_t whole = a.held.first(at.row, at.head, a.Hk) + at.base / kBlock;
-  const int group = (int)(at.base & (kBlock - 1)) / kGroup, u = group >> 1, half = group & 1;
-  uint8_t* const values = a.held.data + whole * a.held.block_bytes + a.held.block_bytes / 2;
-  for (int d = lane; d < D; d += 64) {
-    union {
-      One one[kGroup];
-      Words words;
-      Pair pair;
-    } x;
+  // the group's place in its block (some position of it is inside, so its base is not negative)
+  const int64_t block_of = at.base / kBlock;
+  const int token = (int)(at.base & (kBlock - 1)) + (lane >> 3), u = token / 16, half = token / 8 & 1;
+  for (int32_t head0 = wave; head0 < a.Hk; head0 += kMoveWaves * kHeads) {
+    Eight k[kHeads][kPieces], v[kHeads][kPieces];
+    Tokens old[kHeads][kColumns];
 #pragma unroll
-    for (int i = 0; i < kGroup; ++i) x.one[i] = turned[wave][i][d];
-    const int dt = d / 32, dd = d & 31;
-    One* const to = FP8 ? reinterpret_cast<One*>(values + ((dt * 2 + half) * 32 + dd) * 16 + u * 8)
-                        : reinterpret_cast<One*>(values + (((dt * 2 + u) * 2 + half) * 32 + dd) * 16);
-    if (lives == ~0ull) {
-      if constexpr (FP8) *reinterpret_cast<Pair*>(to) = x.pair;
-      else *reinterpret_cast<Words*>(to) = x.words;
-    } else {
+    for (int h = 0; h < kHeads; ++h) {
+      const int32_t head = head0 + h * kMoveWaves;
+      if (head >= a.Hk) continue;
 #pragma unroll
-      for (int i = 0; i < kGroup; ++i)
-        if (lives >> (8 * i) & 1) to[i] = x.one[i];
+      for (int x = 0; x < kPieces; ++x) {
+        const int d = ((lane & 7) + 8 * x) * 8;
+        k[h][x] = v[h][x] = Eight{};
+        if (live && d < D) {
+          k[h][x] = *reinterpret_cast<const Eight*>(static_cast<const typename T::One*>(a.k.data) + at.row * a.k.row_stride + t * a.k.token_stride + head * a.k.head_stride + d);
+          v[h][x] = *reinterpret_cast<const Eight*>(static_cast<const typename T::One*>(a.v.data) + at.row * a.v.row_stride + t * a.v.token_stride + head * a.v.head_stride + d);
+        }
+      }
+      if (lives != ~0ull) {
+        const uint8_t* const values = a.held.data + (a.held.first(at.row, head, a.Hk) + block_of) * a.held.block_bytes + a.held.block_bytes / 2;
+#pragma unroll
+        for (int x = 0; x < kColumns; ++x)
+          if (lane + 64 * x < D) old[h][x] = *reinterpret_cast<const Tokens*>(values + value_place<FP8>(lane + 64 * x, u, half));
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+      const int32_t head = head0 + h * kMoveWaves;
+      if (head >= a.Hk) continue;
+      const int64_t block = a.held.first(at.row, head, a.Hk) + block_of;
+      uint8_t* const data = a.held.data + block * a.held.block_bytes;
+      float k_down = 1.0f, v_down = 1.0f;
+      if constexpr (FP8) {
+        float k_most = 0, v_most = 0;
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x) {
+          k_most = largest<T>(k[h][x], k_most);
+          v_most = largest<T>(v[h][x], v_most);
+        }
+#pragma unroll
+        for (int r = 1; r < 8; r *= 2) {
+          k_most = fmaxf(k_most, __shfl_xor(k_most, r));
+          v_most = fmaxf(v_most, __shfl_xor(v_most, r));
+        }
+        const uint32_t k_exp = scale_exponent(k_most), v_exp = scale_exponent(v_most);
+        k_down = __uint_as_float((254 - k_exp) << 23);
+        v_down = __uint_as_float((254 - v_exp) << 23);
+        if (live && (lane & 7) == 0) {
+          uint8_t* const scale = a.held.scale + block * kScaleBytes;
+          scale[key_row(token)] = (uint8_t)k_exp;
+          scale[kBlock + token] = (uint8_t)v_exp;
+        }
+      }
+      turn_sync();                                       // (the last head's have been read)
+#pragma unroll
+      for (int x = 0; x < kPieces; ++x) {
+        const int piece = (lane & 7) + 8 * x;
+        if (piece * 8 >= D) continue;
+        if constexpr (FP8) {
+          if (live) *reinterpret_cast<Pair*>(data + key_place<FP8>(piece, token)) = to_fp8<T>(k[h][x], k_down);
+          *reinterpret_cast<Pair*>(&turned[wave][lane >> 3][piece * 8]) = to_fp8<T>(v[h][x], v_down);
+        } else {
+          if (live) *reinterpret_cast<Eight*>(data + key_place<FP8>(piece, token)) = k[h][x];
+          *reinterpret_cast<Eight*>(&turned[wave][lane >> 3][piece * 8]) = v[h][x];
+        }
+      }
+      turn_sync();
+#pragma unroll
+      for (int x = 0; x < kColumns; ++x) {
+        const int d = lane + 64 * x;
+        if (d >= D) continue;
+        union {
+          One one[kGroup];
+          Tokens all;
+        } y;
+        if (lives != ~0ull) y.all = old[h][x];
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i)
+          if (lives >> (8 * i) & 1) y.one[i] = turned[wave][i][d];
+        *reinterpret_cast<Tokens*>(data + a.held.block_bytes / 2 + value_place<FP8>(d, u, half)) = y.all;
+      }
     }
   }
 }
@@ -172,63 +197,86 @@ __global__ __launch_bounds__(64 * kMoveWaves) void cache_write_kernel(MoveArgs a
 template <class T, int D, bool FP8>
 __global__ __launch_bounds__(64 * kMoveWaves) void cache_read_kernel(MoveArgs a) {
   typedef typename T::Eight Eight;
+  typedef typename T::One Value;
   typedef typename Cell<T, FP8>::Type One;
-  constexpr int kPieces = (D / 8 + 7) / 8;
+  typedef typename Cell<T, FP8>::Eight Tokens;
+  constexpr int kPieces = (D / 8 + 7) / 8, kColumns = (D + 63) / 64;
   __shared__ alignas(16) One turned[kMoveWaves][kGroup][D + 16 / sizeof(One)];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t number = blockIdx.x * kMoveWaves + wave;
-  const bool inside = number < (uint32_t)a.rows * a.groups * a.Hk;
-  const Place at(a, inside ? number : 0);
+  const Place at(a);
   const int64_t pos = at.base + (lane >> 3), t = pos - at.start;
-  const bool asked = inside && t >= 0 && t < a.n;        // written, be it with zeros
+  const bool asked = t >= 0 && t < a.n;                  // written, be it with zeros
   const bool live = asked && t < at.count && pos >= 0 && pos < a.held.cap;
-  // (a group of the capacity's last block may pass the capacity, never the block)
   const bool any = __ballot(live) != 0;
-  const int64_t block = a.held.first(at.row, at.head, a.Hk) + (any ? at.base / kBlock : 0);
-  const uint8_t* const data = a.held.data + block * a.held.block_bytes;
-  const uint8_t* const values = data + a.held.block_bytes / 2;
-  const uint8_t* const scale = FP8 ? a.held.scale + block * kScaleBytes : nullptr;
-  const int group = (int)(at.base & (kBlock - 1)) / kGroup, u = group >> 1, half = group & 1;
-  const int in_block = (int)(pos & (kBlock - 1));
-  if (any) {
-    for (int d = lane; d < D; d += 64) {
-      union {
-        One one[kGroup];
-        Words words;
-        Pair pair;
-      } x;
-      const int dt = d / 32, dd = d & 31;
-      if constexpr (FP8) x.pair = *reinterpret_cast<const Pair*>(values + ((dt * 2 + half) * 32 + dd) * 16 + u * 8);
-      else x.words = *reinterpret_cast<const Words*>(values + (((dt * 2 + u) * 2 + half) * 32 + dd) * 16);
+  if (__ballot(asked) == 0) return;
+  // (a group of the capacity's last block may pass the capacity, never the block)
+  const int64_t block_of = any ? at.base / kBlock : 0;
+  const int token = (int)(at.base & (kBlock - 1)) + (lane >> 3), u = token / 16, half = token / 8 & 1;
+  for (int32_t head0 = wave; head0 < a.Hk; head0 += kMoveWaves * kHeads) {
+    Tokens columns[kHeads][kColumns];
+    Pair codes[kHeads][kPieces];
+    Eight k[kHeads][kPieces];
+    uint32_t k_exp[kHeads], v_exp[kHeads];
 #pragma unroll
-      for (int i = 0; i < kGroup; ++i) turned[wave][i][d] = x.one[i];
-    }
-  }
-  __syncthreads();
-  float k_scale = 1.0f, v_scale = 1.0f;
-  if constexpr (FP8) {
-    if (live) {
-      k_scale = __uint_as_float((uint32_t)scale[key_row(in_block)] << 23);
-      v_scale = __uint_as_float((uint32_t)scale[kBlock + in_block] << 23);
-    }
-  }
+    for (int h = 0; h < kHeads; ++h) {
+      const int32_t head = head0 + h * kMoveWaves;
+      if (head >= a.Hk || !any) continue;
+      const int64_t block = a.held.first(at.row, head, a.Hk) + block_of;
+      const uint8_t* const data = a.held.data + block * a.held.block_bytes;
 #pragma unroll
-  for (int x = 0; x < kPieces; ++x) {
-    const int piece = (lane & 7) + 8 * x, d = piece * 8;
-    if (d >= D || !asked) continue;
-    Eight k{}, v{};
-    if (live) {
-      if constexpr (FP8) {
-        k = from_fp8<T>(*reinterpret_cast<const Pair*>(data + (((piece >> 2) * 2 + (piece & 1)) * kBlock + key_row(in_block)) * 16 + (piece >> 1 & 1) * 8), k_scale);
-        v = from_fp8<T>(*reinterpret_cast<const Pair*>(&turned[wave][lane >> 3][d]), v_scale);
-      } else {
-        k = *reinterpret_cast<const Eight*>(data + (piece * kBlock + key_row(in_block)) * 16);
-        v = *reinterpret_cast<const Eight*>(&turned[wave][lane >> 3][d]);
+      for (int x = 0; x < kColumns; ++x)
+        if (lane + 64 * x < D) columns[h][x] = *reinterpret_cast<const Tokens*>(data + a.held.block_bytes / 2 + value_place<FP8>(lane + 64 * x, u, half));
+#pragma unroll
+      for (int x = 0; x < kPieces; ++x) {
+        const int piece = (lane & 7) + 8 * x;
+        if (piece * 8 >= D || !live) continue;
+        if constexpr (FP8) codes[h][x] = *reinterpret_cast<const Pair*>(data + key_place<FP8>(piece, token));
+        else k[h][x] = *reinterpret_cast<const Eight*>(data + key_place<FP8>(piece, token));
+      }
+      if (FP8 && live) {
+        const uint8_t* const scale = a.held.scale + block * kScaleBytes;
+        k_exp[h] = scale[key_row(token)];
+        v_exp[h] = scale[kBlock + token];
       }
     }
-    typedef typename T::One Value;
-    *reinterpret_cast<Eight*>(static_cast<Value*>(const_cast<void*>(a.k.data)) + at.row * a.k.row_stride + t * a.k.token_stride + at.head * a.k.head_stride + d) = k;
-    *reinterpret_cast<Eight*>(static_cast<Value*>(const_cast<void*>(a.v.data)) + at.row * a.v.row_stride + t * a.v.token_stride + at.head * a.v.head_stride + d) = v;
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+      const int32_t head = head0 + h * kMoveWaves;
+      if (head >= a.Hk) continue;
+      turn_sync();                                       // (the last head's have been read)
+      if (any) {
+#pragma unroll
+        for (int x = 0; x < kColumns; ++x) {
+          union {
+            One one[kGroup];
+            Tokens all;
+          } y;
+          y.all = columns[h][x];
+          if (lane + 64 * x < D) {
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) turned[wave][i][lane + 64 * x] = y.one[i];
+          }
+        }
+      }
+      turn_sync();
+#pragma unroll
+      for (int x = 0; x < kPieces; ++x) {
+        const int piece = (lane & 7) + 8 * x, d = piece * 8;
+        if (d >= D || !asked) continue;
+        Eight key{}, value{};
+        if (live) {
+          if constexpr (FP8) {
+            key = from_fp8<T>(codes[h][x], __uint_as_float(k_exp[h] << 23));
+            value = from_fp8<T>(*reinterpret_cast<const Pair*>(&turned[wave][lane >> 3][d]), __uint_as_float(v_exp[h] << 23));
+          } else {
+            key = k[h][x];
+            value = *reinterpret_cast<const Eight*>(&turned[wave][lane >> 3][d]);
+          }
+        }
+        *reinterpret_cast<Eight*>(static_cast<Value*>(const_cast<void*>(a.k.data)) + at.row * a.k.row_stride + t * a.k.token_stride + head * a.k.head_stride + d) = key;
+        *reinterpret_cast<Eight*>(static_cast<Value*>(const_cast<void*>(a.v.data)) + at.row * a.v.row_stride + t * a.v.token_stride + head * a.v.head_stride + d) = value;
+      }
+    }
   }
 }
 
@@ -244,8 +292,8 @@ void of_dim(int32_t head_dim, F f) {
 
 template <bool READ>
 void cache_move(const MoveArgs& a, int32_t head_dim, bool f16, bool fp8, hipStream_t st) {
-  // as many rows a launch as keep its threads below 2^32 (a row's waves are 2^25 and a few at most)
-  const int64_t waves = (int64_t)a.groups * a.Hk, most = ((int64_t)1 << 25) / waves + 1;
+  // as many rows a launch as keep its threads below 2^32 (a row's groups are 2^21 and a few at most)
+  const int64_t most = ((int64_t)1 << 23) / a.groups;
   for (int64_t r = 0; r < a.rows; r += most) {
     MoveArgs b = a;
     b.rows = a.rows - r < most ? a.rows - r : most;
@@ -255,7 +303,7 @@ void cache_move(const MoveArgs& a, int32_t head_dim, bool f16, bool fp8, hipStre
     if (a.counts) b.counts += r;
     b.k.data = static_cast<const uint16_t*>(a.k.data) + r * a.k.row_stride;
     b.v.data = static_cast<const uint16_t*>(a.v.data) + r * a.v.row_stride;
-    const uint32_t grid = (uint32_t)((b.rows * waves + kMoveWaves - 1) / kMoveWaves);
+    const uint32_t grid = (uint32_t)(b.rows * a.groups);
     of_dim(head_dim, [&](auto dim) {
       constexpr int D = dim();
       auto* kernel = READ ? (f16 ? (fp8 ? cache_read_kernel<F16, D, true> : cache_read_kernel<F16, D, false>)
