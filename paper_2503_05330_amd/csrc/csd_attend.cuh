@@ -2,12 +2,12 @@
 //
 // A wave holds a tile of 32 query rows as columns of S^T = K Q^T and O^T += V^T P^T, and goes through blocks of 32 tokens.
 // In that orientation a lane's registers belong to one query row (two lanes a row, one for each half of a
-// block's tokens), so the running maximum m and sum l of the softmax, in base 2, are a register each, and rescaling
+// block's tokens), so the running (near) maximum m and sum l of the softmax, in base 2, are a register each, and rescaling
 // O by 2^(m_old - m_new) needs no exchange; two lanes exchange one value per block for the maximum.
 //
 // 8-bit values are multiplied without their scales 2^e, which go into P: P 2^e is as exact in bfloat16 as P.  Half precision
 // has not the range: there the exponent is added to the score, x = s + e, so that P = 2^(x - m) with m the maximum of x
-// is at most 1 whatever the scales are, and l sums P 2^-e.  Keys' scales go into the conversion to 16 bits, which takes a
+// is at most 2^8 whatever the scales are, and l sums P 2^-e.  Keys' scales go into the conversion to 16 bits, which takes a
 // power of two a lane.
 //
 // Sums, maxima and O are in 32 bits.  P is rounded to the 16-bit type, to nearest, for the second product (the matrix
@@ -52,6 +52,7 @@ template <class T, int D, bool FP8>
 struct Wave {
   typedef typename T::Eight Eight;
   static constexpr int kTiles = D / 32;                  // of O's rows
+  static constexpr float kSlack = 8;
 
   Acc o[kTiles];
   Eight q[D / 16];
@@ -112,13 +113,14 @@ struct Wave {
         if constexpr (EDGE) s[e][r] = token_of(r, half) < sees[e] ? s[e][r] : kNone;
         most = fmaxf(most, s[e][r]);
       }
-    most = fmaxf(m, kAdded ? both_max(most) : both_max(most) * scale);
-    if (__ballot(most > m)) {                            // (m -inf: nothing has been summed)
-      const float down = m == kNone ? 0.0f : exp2_fast(m - most);
+    most = kAdded ? both_max(most) : both_max(most) * scale;
+    // m is the maximum when it was last set: weights may grow to 2^kSlack before O is rescaled, which few blocks behind the first do
+    if (__ballot(most > m + kSlack)) {                   // (m -inf: nothing has been summed)
+      const float high = fmaxf(m, most), down = m == kNone ? 0.0f : exp2_fast(m - high);
       l *= down;
 #pragma unroll
       for (int x = 0; x < kTiles; ++x) o[x] *= down;
-      m = most;
+      m = high;
     }
     const float base = m == kNone ? 0.0f : m;
 #pragma unroll

@@ -180,24 +180,22 @@ __device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, const uint8_t*
   const int32_t mine = in_all > turn ? (in_all - turn + turns - 1) / turns : 0;
   const int32_t rounds = kShared ? (in_all + turns - 1) / turns : mine;       // (all waves meet equally often)
   const int32_t whole = run.whole() / kRound;            // rounds of blocks that all rows see whole
+  // the blocks of the round that is loaded next
+  const uint8_t *next_block[kRound], *next_scale[kRound];
   auto load_keys = [&](int32_t j, int32_t stage) {
 #pragma unroll
     for (int e = 0; e < kRound; ++e) {
       const int32_t x = (turn + j * turns) * kRound + e;
       bool path;
       const int64_t at = run.place(x < blocks ? x : blocks - 1, &path);       // (the same number of loads in every round)
-      R::template keys<C>(lds + (stage * kRound + e) * Block::kBytes, (path ? run.path.data : run.prompt.data) + at * kBlockBytes,
-                          (path ? run.path.scale : run.prompt.scale) + (FP8 ? at * kScaleBytes : 0), group, w.lane);
+      next_block[e] = uniform((path ? run.path.data : run.prompt.data) + at * kBlockBytes);
+      next_scale[e] = FP8 ? uniform((path ? run.path.scale : run.prompt.scale) + at * kScaleBytes) : nullptr;
+      R::template keys<C>(lds + (stage * kRound + e) * Block::kBytes, next_block[e], next_scale[e], group, w.lane);
     }
   };
-  auto load_values = [&](int32_t j, int32_t stage) {
+  auto load_values = [&](int32_t stage) {                // of the round whose keys were loaded last
 #pragma unroll
-    for (int e = 0; e < kRound; ++e) {
-      const int32_t x = (turn + j * turns) * kRound + e;
-      bool path;
-      const int64_t at = run.place(x < blocks ? x : blocks - 1, &path);
-      R::template values<C>(lds + (stage * kRound + e) * Block::kBytes, (path ? run.path.data : run.prompt.data) + at * kBlockBytes, group, w.lane);
-    }
+    for (int e = 0; e < kRound; ++e) R::template values<C>(lds + (stage * kRound + e) * Block::kBytes, next_block[e], group, w.lane);
   };
   // until the loads before the newest (kStages - 1) rounds' and MORE are done, if so many have been issued behind them
   constexpr int kKeyLoads = kRound * (R::template pieces<C>() + (FP8 ? 1 : 0)), kValueLoads = kRound * R::template pieces<C>();
@@ -208,7 +206,7 @@ __device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, const uint8_t*
   };
   for (int32_t j = 0; j < kStages && j < mine; ++j) {
     load_keys(j, j);
-    if (!kShared || j < kStages - 1) load_values(j, j);
+    if (!kShared || j < kStages - 1) load_values(j);
   }
   queries();
   // (with the builtin, so that the compiler knows: it would wait for the queries, and so for all loads, in every round)
@@ -238,7 +236,7 @@ __device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, const uint8_t*
     wait(j + kStages - 1 < mine, std::integral_constant<int, kShared ? 0 : kValueLoads>{});
     if constexpr (kShared) {
       meet();                                            // the keys are there, and all are done with the last round's values
-      if (j + kStages - 1 < mine) load_values(j + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+      if (j + kStages - 1 < mine) load_values(stage == 0 ? kStages - 1 : stage - 1);
     }
     if (here) {
 #pragma unroll
@@ -259,7 +257,7 @@ __device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, const uint8_t*
       for (int e = 0; e < kRound; ++e) met |= w.template values<kEdge>(s[e], b[e], seen_all[e], seen_any[e]);
     }
     if constexpr (!kShared) {
-      if (j + kStages < mine) load_values(j + kStages, stage);
+      if (j + kStages < mine) load_values(stage);
     }
     stage = stage + 1 == kStages ? 0 : stage + 1;
   };
@@ -378,11 +376,12 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
   if (!prompt && valid) sees = all = most = clamped(path_len - count + nth + 1, path_len);
   auto queries = [&] {
     const One* from = static_cast<const One*>(a.q.data) + ((int64_t)p * a.N + path_of) * a.q.row_stride + t * a.q.token_stride + (head * a.G + g) * a.q.head_stride;
-    const uint32_t flip = a.scale < 0 ? 0x80008000u : 0u;
+    const bool read = valid && a.scale != 0;
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
       Words x{};
-      if (valid && a.scale != 0) x = *reinterpret_cast<const Words*>(from + 16 * c + 8 * w.half) ^ flip;
+      if (read) x = *reinterpret_cast<const Words*>(from + 16 * c + 8 * w.half);
+      if (a.scale < 0) x ^= 0x80008000u;
       w.q[c] = __builtin_bit_cast(Eight, x);
     }
   };
@@ -470,7 +469,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
         float4 y;
         float* z = &y.x;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) z[r] = sum == 0.0f ? 0.0f : w.o[chunk * (kChunk / 32) + x][4 * j + r] * factor;
+        for (int r = 0; r < 4; ++r) z[r] = w.o[chunk * (kChunk / 32) + x][4 * j + r] * factor;
         *reinterpret_cast<float4*>(&part_of(wave)[lane & 31][32 * x + 8 * j + 4 * w.half]) = y;
       }
     sync();
