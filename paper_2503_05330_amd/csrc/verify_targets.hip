@@ -166,7 +166,18 @@ __global__ __launch_bounds__(64) void targets_join_kernel(TargetArgs a) {
   if (threadIdx.x == 0) give(pick, blockIdx.x, a.tokens, a.probs);
 }
 
-int32_t parts_of(int64_t rows, int32_t vocab) { return 1; }
+// Workgroups of a row.  Few rows of large vocabularies are shared by as many as make some 250 of 100000 logits, each of 2048 at
+// least (us in one launch / in two: 8 rows of 152064 20.9 / 7.9, 64 22.5 / 12.9, 128 22.8 / 17.3, 8 of 50257 9.8 / 7.7; but 4
+// rows of 32000 7.8 / 7.4, which the second launch costs a caller, and 2 of 16000 5.9 / 6.9).  Many rows of more than half a megabyte, logits and noise, are cut in
+// eight, so that the last ones leave no CU idle (1088 rows of 152064 with noise 182 / 165, 768 126 / 119; 768 without
+// noise 52 / 63).
+constexpr int32_t kMostParts = 32, kLeastLogits = 2048, kLongParts = 8;
+int32_t parts_of(int64_t rows, int32_t vocab, int64_t bytes) {
+  if (rows >= 512) return bytes * vocab >= 1 << 19 ? kLongParts : 1;
+  int64_t parts = 256 * (int64_t)vocab / 100000 / rows;
+  if (parts > vocab / kLeastLogits) parts = vocab / kLeastLogits;
+  return vocab < 40000 || parts < 1 ? 1 : parts > kMostParts ? kMostParts : (int32_t)parts;
+}
 
 template <class E, bool NOISE>
 void targets(const TargetArgs& a, hipStream_t st) {
@@ -183,7 +194,7 @@ extern "C" {
 int csd_targets_bytes(int64_t rows, int32_t vocab, size_t* out_bytes) {
   using namespace csd::verify;
   if (!out_bytes || rows <= 0 || rows > CSD_MAX_TARGET_ROWS || vocab <= 0 || vocab > CSD_MAX_VOCAB) return CSD_ERR_INVALID_ARG;
-  const int32_t parts = parts_of(rows, vocab);
+  const int32_t parts = parts_of(rows, vocab, 8);        // (the most that the call may want)
   *out_bytes = parts > 1 ? (size_t)rows * parts * sizeof(Pick) : 0;
   return CSD_OK;
 }
@@ -201,7 +212,7 @@ int csd_targets(const void* d_logits, int32_t type, int64_t rows, int32_t vocab,
   if (logit_stride < 0 || (d_noise && noise_stride < 0)) return CSD_ERR_INVALID_ARG;
   if (!(inv_temperature > 0) || inv_temperature > 3.4e38f) return CSD_ERR_INVALID_ARG;
   if (needed && (!d_scratch || scratch_bytes < needed || reinterpret_cast<uintptr_t>(d_scratch) % 16)) return CSD_ERR_WORKSPACE;
-  const int32_t parts = parts_of(rows, vocab);
+  const int32_t parts = parts_of(rows, vocab, (int64_t)element + (d_noise ? 4 : 0));
   const TargetArgs a{d_logits, d_noise, logit_stride, noise_stride, rows, vocab, parts, (vocab + parts - 1) / parts, inv_temperature,
                      d_tokens, d_probs, static_cast<Pick*>(d_scratch)};
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -3,8 +3,9 @@
 Between Index.draft and Index.accept (binding.py) the target model sees every path's newest token and the draft
 behind it.  PathCache holds the keys and values of the prompts, which the paths of a problem share, and of the paths, in 16
 bits or quantised to 8 as they are written, and attends to them; targets() turns the logits into the tokens that
-Index.accept compares with, and the probabilities that Index.append and Index.step take.  Argument marshalling only: all
-of it runs in the HIP kernels of libcsd.so, on the current stream.
+Index.accept compares with, and the probabilities that Index.append and Index.step take.  Argument marshalling only, in
+native code (_csd_torch.so) where the arguments are the usual ones: all of it runs in the HIP kernels of libcsd.so, on the
+current stream.
 """
 from __future__ import annotations
 
@@ -34,12 +35,14 @@ class Heads(ctypes.Structure):
 
 
 _lib = None
+_native = None
 
 
 def load() -> ctypes.CDLL:
-    global _lib
+    global _lib, _native
     if _lib is None:
         lib = binding.load()
+        _native = binding._native
         i32, i64, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         cfgp, heads, f32 = ctypes.POINTER(CacheConfig), ctypes.POINTER(Heads), ctypes.c_float
         lib.csd_cache_bytes.argtypes = [cfgp, ctypes.POINTER(size)]
@@ -113,6 +116,13 @@ class PathCache:
         self._ws = (self._buf.data_ptr() + 255) // 256 * 256
         _check(load().csd_cache_create(ctypes.byref(self.cfg), self._ws, nbytes.value, _stream(), ctypes.byref(self._h)),
                "csd_cache_create")
+        self._sizes = (-1 if self.device.index is None else self.device.index, n_problems, n_paths, n_heads, n_kv_heads, head_dim,
+                       TYPES[dtype])
+        self._scale = head_dim ** -0.5
+
+    def _cache(self):
+        """What every native call starts with."""
+        return self._h.value if self._h else 0, _stream(), *self._sizes
 
     def close(self):
         if getattr(self, "_h", None):
@@ -126,6 +136,9 @@ class PathCache:
             pass
 
     def _write(self, call, what, lead, layer, k, v, start, counts):
+        rc = _native.cache_write(*self._cache(), len(lead) == 1, layer, k, v, start, counts)
+        if rc is not None:
+            return _check(rc, what)
         c, rows = self.cfg, 1
         for x in lead:
             rows *= x
@@ -139,13 +152,17 @@ class PathCache:
     def write(self, layer, k, v, start=None, counts=None):
         """k, v [P][N][n][kv heads][head_dim] to positions start [P][N] int32 (None: 0) and on of the paths, the first counts
         [P][N] int32 of them (None: n).  Whatever was there is replaced."""
-        self._write(load().csd_cache_write, "csd_cache_write", (self.P, self.N), layer, k, v, start, counts)
+        self._write(_lib.csd_cache_write, "csd_cache_write", (self.P, self.N), layer, k, v, start, counts)
 
     def write_prompt(self, layer, k, v, start=None, counts=None):
         """k, v [P][n][kv heads][head_dim] to the prompts; start, counts [P]."""
-        self._write(load().csd_cache_write_prompt, "csd_cache_write_prompt", (self.P,), layer, k, v, start, counts)
+        self._write(_lib.csd_cache_write_prompt, "csd_cache_write_prompt", (self.P,), layer, k, v, start, counts)
 
     def _read(self, call, what, lead, layer, n, start, counts):
+        got = _native.cache_read(*self._cache(), len(lead) == 1, layer, n, start, counts)
+        if got is not None:
+            _check(got[0], what)
+            return got[1], got[2]
         c, rows = self.cfg, 1
         for x in lead:
             rows *= x
@@ -156,11 +173,11 @@ class PathCache:
 
     def read(self, layer, n, start=None, counts=None):
         """Keys and values [P][N][n][kv heads][head_dim] of the paths, rows as in write(); zero beyond a row's count."""
-        return self._read(load().csd_cache_read, "csd_cache_read", (self.P, self.N), layer, n, start, counts)
+        return self._read(_lib.csd_cache_read, "csd_cache_read", (self.P, self.N), layer, n, start, counts)
 
     def read_prompt(self, layer, n, start=None, counts=None):
         """... [P][n][kv heads][head_dim] of the prompts."""
-        return self._read(load().csd_cache_read_prompt, "csd_cache_read_prompt", (self.P,), layer, n, start, counts)
+        return self._read(_lib.csd_cache_read_prompt, "csd_cache_read_prompt", (self.P,), layer, n, start, counts)
 
     def attend(self, layer, q, prompt_len, path_len, counts=None, scale=None, out=None, lse=None, prompt_bound=0, path_bound=0):
         """Attention of q [P][N][n][heads][head_dim], the paths' newest tokens (counts [P][N] of the n; None: all), to their prompts'
@@ -168,6 +185,12 @@ class PathCache:
         Token t of a path sees path_len - count + t + 1 of these.  Returns [P][N][n][heads][head_dim]; lse: a float32 tensor
         [P][N][n][heads] that takes the logarithms of the sums.  scale: 1 / sqrt(head_dim) where None.  prompt_bound,
         path_bound: what no length exceeds (0: the capacities), for the shape of the launch alone."""
+        if out is None and lse is None:
+            got = _native.attend(*self._cache(), layer, q, prompt_len, path_len, counts, self._scale if scale is None else scale,
+                                 prompt_bound, path_bound)
+            if got is not None:
+                _check(got[0], "csd_attend")
+                return got[1]
         c, rows = self.cfg, self.P * self.N
         heads = _heads(q, self.dtype, (self.P, self.N), c.n_heads, c.head_dim)
         n = q.shape[2]
@@ -175,7 +198,7 @@ class PathCache:
             out = torch.empty((self.P, self.N, n, c.n_heads, c.head_dim), dtype=self.dtype, device=self.device)
         _check(load().csd_attend(self._h, layer, ctypes.byref(heads), _ptr(prompt_len, torch.int32, self.P),
                                  _ptr(path_len, torch.int32, rows), _ptr(counts, torch.int32, rows), n,
-                                 c.head_dim ** -0.5 if scale is None else scale, prompt_bound, path_bound,
+                                 self._scale if scale is None else scale, prompt_bound, path_bound,
                                  _ptr(out, self.dtype, rows * n * c.n_heads * c.head_dim),
                                  _ptr(lse, torch.float32, rows * n * c.n_heads), _stream()), "csd_attend")
         return out
@@ -190,6 +213,11 @@ def targets(logits: torch.Tensor, noise: Optional[torch.Tensor] = None, inv_temp
     """The model's tokens and their probabilities from logits [..., vocab] (bfloat16, float16, float32): tokens int32 [...], probs
     float32 [...].  Greedy, or a sample where noise [..., vocab] float32 (-ln(-ln u), u uniform) is given: the largest logit *
     inv_temperature + noise, the lowest of equals.  The probability is that of softmax(logits * inv_temperature)."""
+    load()
+    got = _native.targets(_stream(), logits, noise, inv_temperature)
+    if got is not None:
+        _check(got[0], "csd_targets")
+        return got[1], got[2]
     if logits.dtype not in TYPES:
         raise TypeError("logits of dtype %s" % logits.dtype)
     if noise is not None and (noise.dtype != torch.float32 or noise.shape != logits.shape):

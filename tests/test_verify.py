@@ -414,7 +414,7 @@ def check_targets(logits, noise=None, inv_temperature=1.0):
 
 @pytest.mark.parametrize("dtype", [BF, F16, F32])
 @pytest.mark.parametrize("noisy", [False, True])
-@pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (2, 7), (5, 8), (4, 1000), (3, 4099), (2, 32000), (1, 152064), (600, 777)])
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (2, 7), (5, 8), (4, 1000), (3, 4099), (2, 32000), (1, 152064), (600, 777), (7, 60001), (520, 152064)])
 def test_targets(gen, dtype, noisy, rows, vocab):
     print(dtype, noisy, rows, vocab, flush=True)
     x = (normal(gen, (rows, vocab), F32) * 3).to(dtype)
@@ -456,3 +456,35 @@ def test_ties_infinities_and_rows_without_a_token(gen):
     noise = normal(gen, x.shape, F32)
     noise[0, 3], noise[1, 4], noise[9, 2] = inf, nan, inf
     check_targets(x, noise, 1.0)
+
+
+def test_calls_in_native_code_and_in_python_do_the_same(gen, monkeypatch):
+    class Never:
+        def __getattr__(self, name):
+            return lambda *args: None
+    c = verify.PathCache(2, 3, 70, 50, 8, 2, 64, 4, n_layers=2, fp8=True)
+    kv = normal(gen, (2, 3, 9, 6, 64), BF)
+    k, v = kv[..., 2:4, :], kv[..., 4:, :]
+    pk = normal(gen, (2, 90, 2, 64), BF)[:, 10:80]
+    q, start = normal(gen, (2, 3, 4, 8, 64), BF), ints([[0, 5, 41], [7, 8, 30]])
+    counts, length = ints([[9, 4, 9], [0, 9, 1]]), ints([[9, 9, 50], [8, 17, 31]])
+    logits, noise = normal(gen, (2, 3, 4, 501), F16)[..., 100:], normal(gen, (2, 3, 4, 501), F32)[..., :401]
+
+    def calls():
+        for layer in range(2):
+            for write, shape in ((c.write, (2, 3, 50, 2, 64)), (c.write_prompt, (2, 70, 2, 64))):
+                zero = torch.zeros(shape, dtype=BF, device="cuda")
+                write(layer, zero, zero)
+        c.write(1, k, v, start, counts)
+        c.write_prompt(1, pk, pk.flip(-1), None, ints([70, 33]))
+        yield from c.read(1, 12, start)
+        yield from c.read_prompt(0, 70)
+        yield from c.read_prompt(1, 70, None, ints([50, 70]))
+        yield c.attend(1, q, ints([70, 33]), length, ints([[4, 1, 2], [0, 3, 4]]))
+        yield c.attend(1, q, None, length, None, 0.3, prompt_bound=70, path_bound=50)
+        yield from verify.targets(logits, noise, 0.9)
+        yield from verify.targets(logits.float())
+    native = list(calls())
+    assert verify._native is not None and len(native) == 12
+    monkeypatch.setattr(verify, "_native", Never())
+    assert all(torch.equal(a, b) for a, b in zip(native, calls()))
