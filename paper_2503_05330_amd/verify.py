@@ -213,11 +213,12 @@ def targets(logits: torch.Tensor, noise: Optional[torch.Tensor] = None, inv_temp
     """The model's tokens and their probabilities from logits [..., vocab] (bfloat16, float16, float32): tokens int32 [...], probs
     float32 [...].  Greedy, or a sample where noise [..., vocab] float32 (-ln(-ln u), u uniform) is given: the largest logit *
     inv_temperature + noise, the lowest of equals.  The probability is that of softmax(logits * inv_temperature)."""
-    load()
-    got = _native.targets(_stream(), logits, noise, inv_temperature)
-    if got is not None:
-        _check(got[0], "csd_targets")
-        return got[1], got[2]
+    if logits.is_cuda:
+        load()
+        got = _native.targets(_stream(), logits, noise, inv_temperature)
+        if got is not None:
+            _check(got[0], "csd_targets")
+            return got[1], got[2]
     if logits.dtype not in TYPES:
         raise TypeError("logits of dtype %s" % logits.dtype)
     if noise is not None and (noise.dtype != torch.float32 or noise.shape != logits.shape):
