@@ -1,5 +1,12 @@
 // csd — attention of all paths' new tokens over the cache: a wave's part of it.
 //
+// Blocks in LDS.  Rows of keys lie there as in the cache but for their 16-byte chunks: chunk j of token r is at j ^ swizzle(r), so
+// that the lanes that are served together, with one chunk of 16 tokens or all chunks of 32 d's of a few, touch different
+// banks.  Keys are read as they are, 8 d's of a token a lane; in row m of the product lies the token with bits 2 and 3 of m
+// exchanged: then a lane's registers 8 u .. 8 u + 7 of S^T are tokens 16 u + 8 half .. + 7, the operand P^T of the second
+// product without moving anything between lanes.  Values, of which a lane needs 8 tokens of a d, are turned as they are
+// read (ds_read_b64_tr).
+//
 // A wave holds a tile of 32 query rows as columns of S^T = K Q^T and O^T += V^T P^T, and goes through blocks of 32 tokens.
 // In that orientation a lane's registers belong to one query row (two lanes a row, one for each half of a
 // block's tokens), so the running (near) maximum m and sum l of the softmax, in base 2, are a register each, and rescaling
@@ -36,21 +43,36 @@ __device__ inline float both_sum(float x) {
 // The token of a block that register r (0 .. 15) of a lane's scores belongs to.
 __device__ __host__ constexpr int token_of(int r, int half) { return 16 * (r >> 3) + 8 * half + (r & 7); }
 
-// A block in LDS: keys, values, and the scales of an 8-bit cache, as they lie in the cache.
 template <int D, bool FP8>
-struct Staged {
-  static constexpr int kHalf = kBlock * D * (FP8 ? 1 : 2);             // bytes of the keys
-  static constexpr int kBytes = 2 * kHalf + (FP8 ? kScaleBytes : 0);
-  const uint8_t* at;
-  __device__ Words keys(int c, int lane) const { return *reinterpret_cast<const Words*>(at + c * 1024 + lane * 16); }
-  typedef typename std::conditional<FP8, Pair, Words>::type Values;    // eight tokens' of a d
-  __device__ Values values(int c, int lane) const { return reinterpret_cast<const Values*>(at + kHalf)[c * 64 + lane]; }
-  __device__ const uint8_t* scales() const { return at + 2 * kHalf; }
+struct Rows {
+  static constexpr int kRow = D * (FP8 ? 1 : 2);                       // bytes of a token's keys
+  static constexpr int kHalf = kBlock * kRow;                          // of a block's
+  static constexpr int kChunks = kRow / 16;
+  static constexpr bool kSwizzled = (kChunks & (kChunks - 1)) == 0;    // (rows of 96 and 192 bytes spread over the banks by themselves)
+  static constexpr int log2(int x) { return x <= 1 ? 0 : 1 + log2(x / 2); }
+  // 256 bytes are served at once: bits of r that tell rows within them are passed over; of the others the lowest choose
+  // between the 64 (8-bit: 32) bytes that hold 32 d's, the rest among their chunks.  Linear in the bits of r; bit 4 is not used.
+  static constexpr int swizzle(int r) {
+    if (!kSwizzled) return 0;
+    constexpr int kBits = log2(kChunks < 16 ? kChunks : 16), kInside = FP8 ? 1 : 2, kPassed = log2(kChunks < 16 ? 16 / kChunks : 1);
+    const int q = r >> kPassed;
+    return (q & ((1 << (kBits - kInside)) - 1)) << kInside | (q >> (kBits - kInside) & ((1 << kInside) - 1));
+  }
+  // the 1 KB pieces that a block's keys (values) are copied in: lane i of piece p takes the 16 bytes at 1024 p + source(i) ^ turn(p)
+  static constexpr int kPieces = kHalf / 1024;
+  static __device__ uint32_t source(int lane) { return kSwizzled ? (uint32_t)lane * 16 ^ (uint32_t)swizzle(lane / kChunks) << 4 : (uint32_t)lane * 16; }
+  static __device__ uint32_t turn(int p) { return kSwizzled ? (uint32_t)swizzle(p * (64 / kChunks)) << 4 : 0; }
 };
+
+template <class X>
+__device__ inline X lds_read(uint32_t at) {
+  return *(const __attribute__((address_space(3))) X*)(uintptr_t)at;
+}
 
 template <class T, int D, bool FP8>
 struct Wave {
   typedef typename T::Eight Eight;
+  typedef Rows<D, FP8> R;
   static constexpr int kTiles = D / 32;                  // of O's rows
   static constexpr float kSlack = 8;
 
@@ -59,12 +81,23 @@ struct Wave {
   float m, l;                                            // of the lane's query row; l of its half of the tokens
   float scale;                                           // times log2(e), positive: the queries take the sign, or are zero
   int lane, half;
+  uint32_t own_token, own_keys, own_values[2];           // the token of the lane's row of S^T; where the lane reads in a block
 
   __device__ void begin(float scale_log2) {
     lane = threadIdx.x & 63;
     half = lane >> 5;
     // (a half-precision key of 8 bits times its scale may come out as 65536, so they are converted to half of it)
     scale = (scale_log2 == 0 ? 1.0f : fabsf(scale_log2)) * (FP8 && is_half() ? 2.0f : 1.0f);
+    const int row = lane & 31, token = (row & 19) | (row & 4) << 1 | (row & 8) >> 1;
+    own_token = token;
+    own_keys = token * R::kRow + ((half ^ R::swizzle(token)) << 4);
+    // sixteen lanes read eight (16-bit: four) tokens of 16 d's, 8 bytes each, and have a d's tokens then; 16-bit: twice
+    const int s = lane & 15, wide = lane >> 4 & 1;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int from = 8 * half + (FP8 ? s >> 1 : 4 * r + (s >> 2)), chunk = FP8 ? wide : 2 * wide + (s >> 1 & 1);
+      own_values[r] = from * R::kRow + ((chunk ^ R::swizzle(from)) << 4) + (s & 1) * 8;
+    }
     m = kNone;
     l = 0;
 #pragma unroll
@@ -72,20 +105,21 @@ struct Wave {
   }
   static constexpr bool is_half() { return T::kExponent == F16::kExponent; }
 
-  // S^T of a block
-  __device__ Acc scores(const Staged<D, FP8>& b) const {
+  // S^T of the block at `b`
+  __device__ Acc scores(uint32_t b, uint32_t scales) const {
     Acc s{};
+    const uint32_t at = b + own_keys;
     if constexpr (FP8) {
-      const float key_scale = __uint_as_float(((uint32_t)b.scales()[lane & 31] - (is_half() ? 1 : 0)) << 23);
+      const float key_scale = __uint_as_float(((uint32_t)lds_read<uint8_t>(scales + own_token) - (is_half() ? 1 : 0)) << 23);
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
-        const Words w = b.keys(c, lane);
+        const Words w = lds_read<Words>(R::kSwizzled ? at ^ c << 5 : at + 32 * c);
         s = T::mfma(from_fp8<T>(Pair{w[0], w[1]}, key_scale), q[2 * c], s);
         s = T::mfma(from_fp8<T>(Pair{w[2], w[3]}, key_scale), q[2 * c + 1], s);
       }
     } else {
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) s = T::mfma(__builtin_bit_cast(Eight, b.keys(c, lane)), q[c], s);
+      for (int c = 0; c < D / 16; ++c) s = T::mfma(lds_read<Eight>(R::kSwizzled ? at ^ c << 5 : at + 32 * c), q[c], s);
     }
     return s;
   }
@@ -93,12 +127,12 @@ struct Wave {
   // Scores of PER blocks to weights (times their values' scales), with the running maximum and sum.  EDGE: the row sees a block's first
   // `sees` tokens.
   template <bool EDGE, int PER>
-  __device__ void softmax(Acc (&s)[PER], const Staged<D, FP8> (&b)[PER], const int32_t (&sees)[PER]) {
+  __device__ void softmax(Acc (&s)[PER], const uint32_t (&scales)[PER], const int32_t (&sees)[PER]) {
     uint32_t exps[PER][4];                               // of the lane's 16 tokens' values
     if constexpr (FP8) {
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
-        const Pair lo = *reinterpret_cast<const Pair*>(b[e].scales() + kBlock + 8 * half), hi = *reinterpret_cast<const Pair*>(b[e].scales() + kBlock + 16 + 8 * half);
+        const Pair lo = lds_read<Pair>(scales[e] + kBlock + 8 * half), hi = lds_read<Pair>(scales[e] + kBlock + 16 + 8 * half);
         exps[e][0] = lo[0], exps[e][1] = lo[1], exps[e][2] = hi[0], exps[e][3] = hi[1];
       }
     }
@@ -143,7 +177,23 @@ struct Wave {
       }
   }
 
-  typedef typename Staged<D, FP8>::Values Values;
+  typedef typename std::conditional<FP8, Pair, Words>::type Values;    // eight tokens' of a d
+  // tokens 16 u + 8 half .. + 7 of d 32 x + (lane & 31), of the values at `b`
+  __device__ Values turned(uint32_t b, int x, int u) const {
+    typedef int __attribute__((ext_vector_type(2))) Two;
+    typedef short __attribute__((ext_vector_type(4))) Four;
+    auto at = [&](int r) {
+      const uint32_t y = b + own_values[r];
+      return (R::kSwizzled ? y ^ x << (FP8 ? 5 : 6) : y + (x << (FP8 ? 5 : 6))) + u * 16 * R::kRow;
+    };
+    if constexpr (FP8) {
+      return __builtin_bit_cast(Pair, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) Two*)(uintptr_t)at(0)));
+    } else {
+      const Pair lo = __builtin_bit_cast(Pair, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four*)(uintptr_t)at(0)));
+      const Pair hi = __builtin_bit_cast(Pair, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four*)(uintptr_t)at(1)));
+      return Words{lo[0], lo[1], hi[0], hi[1]};
+    }
+  }
   static constexpr int kWords = FP8 ? 2 : 4;
   __device__ static Eight value_operand(Values w) {
     if constexpr (FP8) return from_fp8<T>(w, 1.0f);
@@ -181,7 +231,7 @@ struct Wave {
   // 0 x infinity would reach the rows that do not see a token, so infinities and NaN of such tokens are left to odd_values();
   // returned is whether the lane has met any.
   template <bool EDGE>
-  __device__ bool values(const Acc& s, const Staged<D, FP8>& b, int32_t all, int32_t most) {
+  __device__ bool values(const Acc& s, uint32_t b, int32_t all, int32_t most) {
     Eight p[2];
     weights(s, p);
     if constexpr (EDGE) {
@@ -193,7 +243,7 @@ struct Wave {
         for (int x = 0; x < kTiles; ++x)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const Values w = b.values(2 * x + u, lane), strange = odd(w) & seen[u] & ~sure[u];
+            const Values w = turned(b, x, u), strange = odd(w) & seen[u] & ~sure[u];
 #pragma unroll
             for (int i = 0; i < kWords; ++i) met |= strange[i];
             o[x] = T::mfma(value_operand(w & seen[u] & ~strange), p[u], o[x]);
@@ -206,24 +256,23 @@ struct Wave {
     for (int x = 0; x < kTiles; ++x)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const Values w = b.values(2 * x + u, lane);
+        const Values w = turned(b, x, u);
         o[x] = T::mfma(value_operand(EDGE ? w & seen[u] : w), p[u], o[x]);
       }
     return false;
   }
   // What values() has left out of a block, which is read from memory again: one token after the other, for the rows that see it.
-  __device__ void odd_values(const uint8_t* block, const uint8_t* scales, int32_t sees, int32_t all, int32_t most) {
+  __device__ void odd_values(const uint8_t* keys, const uint8_t* values, const uint8_t* scales, int32_t sees, int32_t all, int32_t most) {
     Acc s{};
-    const Staged<D, FP8> b{block};
-    float key_scale = 1.0f;
-    if constexpr (FP8) key_scale = __uint_as_float(((uint32_t)scales[lane & 31] - (is_half() ? 1 : 0)) << 23);
+    const float key_scale = FP8 ? __uint_as_float(((uint32_t)scales[own_token] - (is_half() ? 1 : 0)) << 23) : 1.0f;
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) {
+    for (int c = 0; c < D / (FP8 ? 32 : 16); ++c) {
+      const Words w = *reinterpret_cast<const Words*>(keys + own_token * R::kRow + 32 * c + 16 * half);
       if constexpr (FP8) {
-        const Words w = b.keys(c / 2, lane);
-        s = T::mfma(from_fp8<T>(c & 1 ? Pair{w[2], w[3]} : Pair{w[0], w[1]}, key_scale), q[c], s);
+        s = T::mfma(from_fp8<T>(Pair{w[0], w[1]}, key_scale), q[2 * c], s);
+        s = T::mfma(from_fp8<T>(Pair{w[2], w[3]}, key_scale), q[2 * c + 1], s);
       } else {
-        s = T::mfma(__builtin_bit_cast(Eight, b.keys(c, lane)), q[c], s);
+        s = T::mfma(__builtin_bit_cast(Eight, w), q[c], s);
       }
     }
 #pragma unroll
@@ -235,15 +284,17 @@ struct Wave {
     Eight p[2];
     weights(s, p);
     for (int32_t token = all < 0 ? 0 : all; token < most && token < kBlock; ++token) {
-      const Values alone[2] = {kept(0, token + 1) & ~kept(0, token), kept(1, token + 1) & ~kept(1, token)};
+      // of an operand's eight tokens this one alone, in the half of the lanes and the product that hold it
+      const int u = token / 16, word = (token & 7) / (FP8 ? 4 : 2), shift = FP8 ? token % 4 * 8 : token % 2 * 16;
+      const bool mine = (token / 8 & 1) == half;
 #pragma unroll
       for (int x = 0; x < kTiles; ++x) {
-        Acc one{};
+        const int d = 32 * x + (lane & 31);
+        const uint32_t bits = FP8 ? values[token * R::kRow + d] : reinterpret_cast<const uint16_t*>(values)[token * D + d];
+        Values w{};
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const Values w = b.values(2 * x + u, lane);
-          one = T::mfma(value_operand(w & odd(w) & alone[u]), p[u], one);
-        }
+        for (int i = 0; i < kWords; ++i) w[i] = mine && i == word ? bits << shift : 0;
+        const Acc one = T::mfma(value_operand(w & odd(w)), u ? p[1] : p[0], Acc{});
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[x][r] += token < sees ? one[r] : 0.0f;
       }

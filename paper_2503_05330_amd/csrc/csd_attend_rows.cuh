@@ -68,22 +68,23 @@ __device__ inline const uint8_t* uniform(const uint8_t* p) {
   return reinterpret_cast<const uint8_t*>((uint64_t)high << 32 | (uint64_t)low);
 }
 
-// N pieces of 1 KB, a lane's 16 bytes at from + piece KB + 16 lane
-template <int N>
-__device__ inline void fetch(uint32_t lds, const uint8_t* from, uint32_t lane_bytes) {
+// N pieces of 1 KB from piece p on
+template <class R, int N>
+__device__ inline void fetch(uint32_t lds, const uint8_t* from, int p, uint32_t source) {
   if constexpr (N >= 4) {
     asm volatile(
-        "s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
-        "global_load_lds_dwordx4 %1, %2 offset:1024\n\tglobal_load_lds_dwordx4 %1, %2 offset:2048\n\t"
-        "global_load_lds_dwordx4 %1, %2 offset:3072" ::"s"(lds), "v"(lane_bytes), "s"(from) : "memory");
-    if constexpr (N > 4) fetch<N - 4>(lds + 4096, from + 4096, lane_bytes);
+        "s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
+        "global_load_lds_dwordx4 %2, %5 offset:1024\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048\n\t"
+        "global_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds), "v"(source ^ R::turn(p)), "v"(source ^ R::turn(p + 1)),
+        "v"(source ^ R::turn(p + 2)), "v"(source ^ R::turn(p + 3)), "s"(from) : "memory");
+    if constexpr (N > 4) fetch<R, N - 4>(lds + 4096, from + 4096, p + 4, source);
   } else if constexpr (N >= 2) {
     asm volatile(
-        "s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
-        "global_load_lds_dwordx4 %1, %2 offset:1024" ::"s"(lds), "v"(lane_bytes), "s"(from) : "memory");
-    if constexpr (N > 2) fetch<N - 2>(lds + 2048, from + 2048, lane_bytes);
+        "s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
+        "global_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds), "v"(source ^ R::turn(p)), "v"(source ^ R::turn(p + 1)), "s"(from) : "memory");
+    if constexpr (N > 2) fetch<R, N - 2>(lds + 2048, from + 2048, p + 2, source);
   } else {
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_bytes), "s"(from) : "memory");
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(source ^ R::turn(p)), "s"(from) : "memory");
   }
 }
 // 64 bytes, 4 from each of the first sixteen lanes
@@ -98,23 +99,21 @@ __device__ inline void wait_loads() {
 }
 __device__ inline void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-__device__ inline uint32_t lds_offset(const void* p) {
-  return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p);
-}
+__device__ inline uint32_t lds_offset(const void* p) { return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p); }
 
 // The sizes of a ring: blocks for two workgroups on a CU where one for each wave leaves room for them.  (Twice the blocks, for launches of
 // no more workgroups than CUs, took 16 paths of 1024 + 1024 tokens from 20.4 to 22.1 us.)
 template <int D, bool FP8>
 struct Ring {
-  typedef Staged<D, FP8> Block;
-  static constexpr int kKeys = Block::kHalf / 1024;      // pieces of the keys, and of the values
+  typedef Rows<D, FP8> R;
+  static constexpr int kBlockBytes = 2 * R::kHalf;       // keys, then values
   static constexpr int blocks() {
     int x = kWaves;
-    while (x * 2 * Block::kBytes <= 72 * 1024) x *= 2;
+    while (x * 2 * (kBlockBytes + kScaleBytes) <= 72 * 1024) x *= 2;
     return x;
   }
   static constexpr int kBlocks = blocks();
-  static constexpr int kBytes = kBlocks * Block::kBytes;
+  static constexpr int kBytes = kBlocks * kBlockBytes;
   static constexpr int kResident = kBytes <= 72 * 1024 && D <= 128 ? 2 : 1;   // workgroups of a CU
   // Where C waves share blocks: how many blocks a round takes, and stages of so many.  (Two where that leaves two stages: an exchange of
   // maxima and two barriers for 64 tokens.  64 paths x 17 tokens of 4096 + 4096: 132 us with one, 122 with two.)
@@ -124,28 +123,20 @@ struct Ring {
   static constexpr int stages() { return kBlocks * C / kWaves / round<C>(); }
   // loads of a wave when C waves share them
   template <int C>
-  static constexpr int pieces() { return (kKeys + C - 1) / C; }
-
-  // The wave's share of the keys (and scales), of the values
+  static constexpr int pieces() { return (R::kPieces + C - 1) / C; }
+  // the wave's share of the keys, or of the values
   template <int C>
-  static __device__ void keys(uint32_t lds, const uint8_t* block, const uint8_t* scale, int group, int lane) {
+  static __device__ void load(uint32_t lds, const uint8_t* block, int group, uint32_t source) {
     constexpr int N = pieces<C>();
-    const uint32_t first = 1024u * (group * N < kKeys - N ? group * N : kKeys - N);
-    fetch<N>(uniform(lds + first), uniform(block + first), lane * 16);
-    if constexpr (FP8) fetch_scales(uniform(lds + 2 * Block::kHalf), uniform(scale), lane);
-  }
-  template <int C>
-  static __device__ void values(uint32_t lds, const uint8_t* block, int group, int lane) {
-    constexpr int N = pieces<C>();
-    const uint32_t first = Block::kHalf + 1024u * (group * N < kKeys - N ? group * N : kKeys - N);
-    fetch<N>(uniform(lds + first), uniform(block + first), lane * 16);
+    const int first = group * N < R::kPieces - N ? group * N : R::kPieces - N;
+    fetch<R, N>(uniform(lds + 1024u * first), uniform(block + 1024u * first), first, source);
   }
 };
 
 // A run of blocks: the prompt's and the path's that all rows of the tile see whole, then those that some row does not see
 // all of.
 struct Segment {
-  const uint8_t *data, *scale;           // of its first block in the run
+  const uint8_t *keys, *values, *scale;  // of its first block in the run
   int32_t first, whole, edge;            // the first block's number, how many blocks are seen whole, how many follow them
 };
 struct Run {
@@ -168,34 +159,32 @@ struct Run {
 // sees; all, most: of the path, that all of the wave's rows, that any of them sees.  queries() loads the wave's queries, while
 // the first blocks are on their way.  Returns whether there are values left for odd_values().
 template <class T, int D, bool FP8, int C, class Queries>
-__device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, const uint8_t* ring, int32_t group, int32_t turn, int32_t turns,
+__device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, uint32_t ring, uint32_t scales, int32_t group, int32_t turn, int32_t turns,
                               int32_t prompt_len, int32_t sees, int32_t all, int32_t most, Queries queries) {
   typedef Ring<D, FP8> R;
-  typedef typename R::Block Block;
-  constexpr int64_t kBlockBytes = 2 * Block::kHalf;
+  constexpr int kHalf = Rows<D, FP8>::kHalf;
   constexpr bool kShared = C > 1;
   constexpr int kRound = R::template round<C>(), kStages = R::template stages<C>();
-  const uint32_t lds = uniform(lds_offset(ring));
+  const uint32_t source = Rows<D, FP8>::source(w.lane);
   const int32_t blocks = run.blocks(), in_all = (blocks + kRound - 1) / kRound;
   const int32_t mine = in_all > turn ? (in_all - turn + turns - 1) / turns : 0;
   const int32_t rounds = kShared ? (in_all + turns - 1) / turns : mine;       // (all waves meet equally often)
   const int32_t whole = run.whole() / kRound;            // rounds of blocks that all rows see whole
-  // the blocks of the round that is loaded next
-  const uint8_t *next_block[kRound], *next_scale[kRound];
+  const uint8_t* next_values[kRound];                    // of the round whose keys were loaded last
   auto load_keys = [&](int32_t j, int32_t stage) {
 #pragma unroll
     for (int e = 0; e < kRound; ++e) {
       const int32_t x = (turn + j * turns) * kRound + e;
       bool path;
       const int64_t at = run.place(x < blocks ? x : blocks - 1, &path);       // (the same number of loads in every round)
-      next_block[e] = uniform((path ? run.path.data : run.prompt.data) + at * kBlockBytes);
-      next_scale[e] = FP8 ? uniform((path ? run.path.scale : run.prompt.scale) + at * kScaleBytes) : nullptr;
-      R::template keys<C>(lds + (stage * kRound + e) * Block::kBytes, next_block[e], next_scale[e], group, w.lane);
+      next_values[e] = uniform((path ? run.path.values : run.prompt.values) + at * kHalf);
+      R::template load<C>(ring + (stage * kRound + e) * R::kBlockBytes, (path ? run.path.keys : run.prompt.keys) + at * kHalf, group, source);
+      if constexpr (FP8) fetch_scales(uniform(scales + (stage * kRound + e) * kScaleBytes), uniform((path ? run.path.scale : run.prompt.scale) + at * kScaleBytes), w.lane);
     }
   };
-  auto load_values = [&](int32_t stage) {                // of the round whose keys were loaded last
+  auto load_values = [&](int32_t stage) {
 #pragma unroll
-    for (int e = 0; e < kRound; ++e) R::template values<C>(lds + (stage * kRound + e) * Block::kBytes, next_block[e], group, w.lane);
+    for (int e = 0; e < kRound; ++e) R::template load<C>(ring + (stage * kRound + e) * R::kBlockBytes + kHalf, next_values[e], group, source);
   };
   // until the loads before the newest (kStages - 1) rounds' and MORE are done, if so many have been issued behind them
   constexpr int kKeyLoads = kRound * (R::template pieces<C>() + (FP8 ? 1 : 0)), kValueLoads = kRound * R::template pieces<C>();
@@ -216,11 +205,12 @@ __device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, const uint8_t*
   auto round = [&](int32_t j, auto edge_of) {
     constexpr bool kEdge = decltype(edge_of)::value;
     const bool here = j < mine;
-    Block b[kRound];
+    uint32_t b[kRound], b_scales[kRound];
     int32_t seen[kRound] = {}, seen_all[kRound] = {}, seen_any[kRound] = {};
 #pragma unroll
     for (int e = 0; e < kRound; ++e) {
-      b[e].at = ring + (stage * kRound + e) * Block::kBytes;
+      b[e] = ring + (stage * kRound + e) * R::kBlockBytes;
+      b_scales[e] = scales + (stage * kRound + e) * kScaleBytes;
       if constexpr (kEdge) {
         const int32_t x = (turn + j * turns) * kRound + e;
         bool path = false;
@@ -240,21 +230,21 @@ __device__ inline bool stream(Wave<T, D, FP8>& w, const Run& run, const uint8_t*
     }
     if (here) {
 #pragma unroll
-      for (int e = 0; e < kRound; ++e) s[e] = w.scores(b[e]);
-      w.template softmax<kEdge, kRound>(s, b, seen);
+      for (int e = 0; e < kRound; ++e) s[e] = w.scores(b[e], b_scales[e]);
+      w.template softmax<kEdge, kRound>(s, b_scales, seen);
     }
     if constexpr (kShared) {
       wait(j + kStages - 1 < mine, std::integral_constant<int, 0>{});
       meet();                                            // the values are there, and all are done with the keys
       if (j + kStages < mine) load_keys(j + kStages, stage);
     } else {
-      // (the scales, which lie behind the keys, have been read by then)
+      // (the scales have been read by then)
       if (j + kStages < mine) load_keys(j + kStages, stage);
       wait(j + kStages < mine, std::integral_constant<int, kKeyLoads>{});
     }
     if (here) {
 #pragma unroll
-      for (int e = 0; e < kRound; ++e) met |= w.template values<kEdge>(s[e], b[e], seen_all[e], seen_any[e]);
+      for (int e = 0; e < kRound; ++e) met |= w.template values<kEdge>(s[e], b[e] + kHalf, seen_all[e], seen_any[e]);
     }
     if constexpr (!kShared) {
       if (j + kStages < mine) load_values(stage);
@@ -285,7 +275,8 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
   __shared__ int32_t packed;
   __shared__ float tops[kWaves][32], sums[kWaves][32];
   __shared__ int32_t places[kWaves][32];
-  __shared__ alignas(16) uint8_t ring[R::kBytes];
+  __shared__ alignas(512) uint8_t ring[R::kBytes];
+  __shared__ alignas(16) uint8_t ring_scales[FP8 ? R::kBlocks * kScaleBytes : 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // the item
@@ -380,7 +371,8 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
       Words x{};
-      if (read) x = *reinterpret_cast<const Words*>(from + 16 * c + 8 * w.half);
+      // (8-bit keys come 16 d's of a half at a time)
+      if (read) x = *reinterpret_cast<const Words*>(from + (FP8 ? c / 2 * 32 + 16 * w.half + c % 2 * 8 : 16 * c + 8 * w.half));
       if (a.scale < 0) x ^= 0x80008000u;
       w.q[c] = __builtin_bit_cast(Eight, x);
     }
@@ -402,7 +394,8 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
     to->first = from;
     to->whole = whole < 0 ? 0 : whole < own ? whole : own;
     to->edge = own - to->whole;
-    to->data = held.data + (at + from) * held.block_bytes;
+    to->keys = held.keys + (at + from) * Rows<D, FP8>::kHalf;
+    to->values = held.values + (at + from) * Rows<D, FP8>::kHalf;
     to->scale = FP8 ? held.scale + (at + from) * kScaleBytes : nullptr;
   };
   if (prompt || a.how == kDirect) part(&run.prompt, a.prompt, a.prompt.first(p, head, a.Hk), prompt ? (int32_t)splits : 1, prompt ? split : 0, prompt_len, prompt_len);
@@ -410,11 +403,13 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
     part(&run.path, a.path, a.path.first(row, head, a.Hk), (int32_t)splits, split, clamped(path_len - count + first / a.G + 1, path_len),
          clamped(path_len - count + (first + here - 1) / a.G + 1, path_len));
   {
-    const uint8_t* own = ring + (solo ? wave : turn) * (R::kBytes / (solo ? kWaves : turns));
+    const int32_t share = solo ? wave : turn, shares = solo ? kWaves : turns;            // of the ring
+    const uint32_t own = uniform(lds_offset(ring) + share * (R::kBytes / shares));
+    const uint32_t own_scales = uniform(lds_offset(ring_scales) + share * (R::kBlocks * kScaleBytes / shares));
     bool odd;
-    if (groups == 1) odd = stream<T, D, FP8, 1>(w, run, own, group, turn, turns, prompt_len, sees, all, most, queries);
-    else if (groups == 2) odd = stream<T, D, FP8, 2>(w, run, own, group, turn, turns, prompt_len, sees, all, most, queries);
-    else odd = stream<T, D, FP8, 4>(w, run, own, group, turn, turns, prompt_len, sees, all, most, queries);
+    if (groups == 1) odd = stream<T, D, FP8, 1>(w, run, own, own_scales, group, turn, turns, prompt_len, sees, all, most, queries);
+    else if (groups == 2) odd = stream<T, D, FP8, 2>(w, run, own, own_scales, group, turn, turns, prompt_len, sees, all, most, queries);
+    else odd = stream<T, D, FP8, 4>(w, run, own, own_scales, group, turn, turns, prompt_len, sees, all, most, queries);
     if (odd) {                                           // (of a path: a prompt's tokens are seen by all or by none)
       const int32_t round = groups == 1 ? R::template round<1>() : groups == 2 ? R::template round<2>() : R::template round<4>();
       for (int32_t x = run.whole() / round * round; x < run.blocks(); ++x) {
@@ -422,7 +417,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
         const int64_t at = run.place(x, &path);
         const int32_t block = kBlock * ((int32_t)at + run.path.first);
         if (path && x / round % turns == turn)
-          w.odd_values(run.path.data + at * a.path.block_bytes, FP8 ? run.path.scale + at * kScaleBytes : nullptr, sees - block, all - block, most - block);
+          w.odd_values(run.path.keys + at * Rows<D, FP8>::kHalf, run.path.values + at * Rows<D, FP8>::kHalf, FP8 ? run.path.scale + at * kScaleBytes : nullptr, sees - block, all - block, most - block);
       }
     }
   }

@@ -1,18 +1,14 @@
 // csd — the cache of keys and values that a verifying pass works on: its layout in memory, and what its kernels share.
 //
-// Layout.  Attention multiplies tiles of 32 tokens on the matrix cores: scores S^T = K Q^T (rows: tokens, columns: query
-// rows), then O^T += V^T P^T, both by v_mfma_f32_32x32x16, whose operands are 8 consecutive values of the contracted
-// axis per lane.  The cache holds blocks of 32 tokens of one head in the order in which a wave's lanes take these
-// operands, so that a copy to LDS is linear and the reads from there are without gaps (eight tokens' values lie together, so a
-// token that is written alone touches the lines of seven others, not those of all 32):
-//   keys    16-bit  [D/16][half][row m][8 d's]          d = 16 c + 8 half + i
-//           8-bit   [D/32][half][row m][2][8 d's]       two operands in a lane's 16 bytes
-//   values  either  [D/32][2][half][32 d's][8 tokens]   token = 16 u + 8 half + i
-// The result S^T leaves tokens 8 j + 4 half + r of its 32 rows in register 4 j + r of a lane.  With keys in row
-// m(token) = the token's bits 2 and 3 exchanged, the lane's registers 8 u .. 8 u + 7 are tokens 16 u + 8 half ..
-// + 7: the operand P^T of the second product without moving anything between lanes.
-// A block is its keys, then its values.  The scales of an 8-bit cache lie in an array of their own, 64 bytes a block: the
-// biased exponents of the 32 tokens' key scales, then of their value scales.
+// Layout.  Keys and values are arrays [row][kv head][tokens][D] of their own, row: a prompt or a path, tokens rounded up to blocks of
+// 32: a token that is written fills whole lines (8-bit heads of 128: one for its keys, one for its values), and no byte of
+// another's.  (In the order of the matrix cores' operands, keys by eights of d's and values by eights of tokens, reads needed no
+// turning, but a token lay in 17 lines: writing one of 64 x 16 paths of 8 heads took 12 us, and 9 tokens 21.)  The scales of
+// an 8-bit cache lie in an array of their own, 64 bytes a block of 32 tokens: the biased exponents of the tokens' key scales,
+// then of their value scales.
+//
+// Attention multiplies tiles of 32 tokens: scores S^T = K Q^T (rows: tokens, columns: query rows), then O^T += V^T P^T, both
+// by v_mfma_f32_32x32x16, whose operands are 8 values of the contracted axis per lane.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -68,17 +64,14 @@ __device__ inline typename T::Eight from_fp8(Pair codes, float scale) {
 
 // One layer's prompts or paths.
 struct Held {
-  uint8_t* data;     // [row][kv head][blocks][block_bytes]
-  uint8_t* scale;    // [row][kv head][blocks][64], 8-bit only
-  int32_t cap;       // tokens of a row
-  int32_t blocks;    // of a row and head
-  int64_t block_bytes;
+  uint8_t *keys, *values;            // [row][kv head][blocks * 32][D]
+  uint8_t* scale;                    // [row][kv head][blocks][64], 8-bit only
+  int32_t cap;                       // tokens of a row
+  int32_t blocks;                    // of a row and head
   __device__ __host__ int64_t first(int64_t row, int32_t head, int32_t heads) const { return (row * heads + head) * blocks; }
 };
 
-constexpr int64_t block_bytes(int64_t head_dim, bool fp8) { return 2 * kBlock * head_dim * (fp8 ? 1 : 2); }
-
-__device__ inline int key_row(int token) { return (token & 19) | (token & 4) << 1 | (token & 8) >> 1; }
+constexpr int64_t block_bytes(int64_t head_dim, bool fp8) { return kBlock * head_dim * (fp8 ? 1 : 2); }   // of the keys, of the values
 
 // What a call of csd_attend hands to its kernels.
 struct AttendArgs {
@@ -110,7 +103,7 @@ struct MoveArgs {
   csd_heads k, v;                    // (read: dense)
   const int32_t *start, *counts;
   int64_t rows;
-  int32_t n, Hk, groups;             // groups of eight cache positions that n tokens touch at most
+  int32_t n, Hk, groups;             // groups of eight of the n tokens
   uint32_t* status;
 };
 

@@ -18,7 +18,7 @@ int64_t aligned_up(int64_t x) { return (x + kWorkspaceAlign - 1) / kWorkspaceAli
 constexpr int64_t kMoreParts = 1 << 16;
 
 struct CacheLayout {
-  int64_t prompt, path, prompt_scale, path_scale, part_o, part_lse, status, total;
+  int64_t prompt_keys, prompt_values, path_keys, path_values, prompt_scale, path_scale, part_o, part_lse, status, total;
   int64_t prompt_layer, path_layer;      // blocks of a layer
   int64_t parts;
 };
@@ -39,7 +39,7 @@ int check(const csd_cache_config* c) {
 
 // false: too large for an address
 bool layout_of(const csd_cache_config* c, CacheLayout* l) {
-  const double bytes = (double)c->n_layers * c->n_problems * c->n_kv_heads * block_bytes(c->head_dim, c->fp8) *
+  const double bytes = (double)c->n_layers * c->n_problems * c->n_kv_heads * 2.0 * block_bytes(c->head_dim, c->fp8) *
                        ((c->prompt_cap + kBlock - 1) / kBlock + (double)c->n_paths * ((c->path_cap + kBlock - 1) / kBlock));
   if (bytes > 1e15) return false;
   const int64_t per_block = block_bytes(c->head_dim, c->fp8);
@@ -52,8 +52,10 @@ bool layout_of(const csd_cache_config* c, CacheLayout* l) {
     *place = at;
     at += aligned_up(size);
   };
-  take(&l->prompt, c->n_layers * l->prompt_layer * per_block);
-  take(&l->path, c->n_layers * l->path_layer * per_block);
+  take(&l->prompt_keys, c->n_layers * l->prompt_layer * per_block);
+  take(&l->prompt_values, c->n_layers * l->prompt_layer * per_block);
+  take(&l->path_keys, c->n_layers * l->path_layer * per_block);
+  take(&l->path_values, c->n_layers * l->path_layer * per_block);
   take(&l->prompt_scale, c->fp8 ? c->n_layers * l->prompt_layer * kScaleBytes : 0);
   take(&l->path_scale, c->fp8 ? c->n_layers * l->path_layer * kScaleBytes : 0);
   take(&l->part_o, l->parts * c->head_dim * 4);
@@ -84,12 +86,11 @@ struct csd_cache {
 
   csd::verify::Held held(bool prompt, int32_t layer) const {
     using namespace csd::verify;
-    const int64_t per_block = block_bytes(cfg.head_dim, cfg.fp8);
-    const int64_t first = layer * (prompt ? layout.prompt_layer : layout.path_layer);
+    const int64_t first = layer * (prompt ? layout.prompt_layer : layout.path_layer), at = first * block_bytes(cfg.head_dim, cfg.fp8);
     const int32_t cap = prompt ? cfg.prompt_cap : cfg.path_cap;
-    return Held{base + (prompt ? layout.prompt : layout.path) + first * per_block,
+    return Held{base + (prompt ? layout.prompt_keys : layout.path_keys) + at, base + (prompt ? layout.prompt_values : layout.path_values) + at,
                 cfg.fp8 ? base + (prompt ? layout.prompt_scale : layout.path_scale) + first * kScaleBytes : nullptr, cap,
-                (cap + kBlock - 1) / kBlock, per_block};
+                (cap + kBlock - 1) / kBlock};
   }
   uint32_t* status() const { return reinterpret_cast<uint32_t*>(base + layout.status); }
 };
@@ -114,8 +115,7 @@ int move(csd_cache* c, bool read, bool prompt, int32_t layer, const csd_heads& k
   a.rows = prompt ? c->cfg.n_problems : (int64_t)c->cfg.n_problems * c->cfg.n_paths;
   a.n = n;
   a.Hk = c->cfg.n_kv_heads;
-  // (rows that start at an aligned position need no group more)
-  a.groups = start ? (n + 14) / 8 : (n + 7) / 8;
+  a.groups = (n + 7) / 8;
   a.status = c->status();
   if (read) cache_read(a, c->cfg.head_dim, c->cfg.type == CSD_F16, c->cfg.fp8, static_cast<hipStream_t>(stream));
   else cache_write(a, c->cfg.head_dim, c->cfg.type == CSD_F16, c->cfg.fp8, static_cast<hipStream_t>(stream));

@@ -1,61 +1,41 @@
 // csd — keys and values written to the cache of a verifying pass, and read back.
 //
-// A workgroup takes eight consecutive cache positions, aligned to eight, of one row; its waves take the kv heads, which lie
-// side by side in a projection's output, two at a time so that twice as much is on its way.  Eight lanes
-// hold a token, 16 bytes each at a time, so that a token's largest value is found in three exchanges.  Keys go from these
-// registers to their place (pieces of eight d's stay together); values, which lie eight tokens together, are turned in the
-// wave's part of LDS.  A value store is 16 (8-bit: 8) bytes: eight positions of a row and head are one wave's, so where not all of
-// them are written the others are read first and written back.
+// A workgroup takes eight tokens of one row, its waves the kv heads, which lie side by side in a projection's output.  Eight
+// lanes hold a token, so that its largest value is found in three exchanges; a lane has 16 values of each 128 of a token,
+// 16 bytes of codes.  Long calls are bound by the copy: 8 prompts of up to 4096 tokens (half of them there), 8 heads of 128, are written
+// to 8 bits in 23.9 us and read back, with zeros for the missing, in 35.9: 4.2 and 4.7 TB/s.  Short ones are bound by the launch
+// and the loads before a row's place is known: 64 x 16 paths of up to 9 tokens, 8 heads of 128, take 15.5 us to 8 bits.
 #include "csd_verify.cuh"
 
 namespace csd {
 namespace verify {
 namespace {
 
-constexpr int kGroup = 8;               // positions of a workgroup
-constexpr int kMoveWaves = 4, kHeads = 2;
+constexpr int kGroup = 8;               // tokens of a workgroup
+constexpr int kMoveWaves = 8;
 
-template <class T, bool FP8>
-struct Cell {
-  typedef uint16_t Type;
-  typedef Words Eight;                  // a d's values of eight tokens
-};
-template <class T>
-struct Cell<T, true> {
-  typedef uint8_t Type;
-  typedef Pair Eight;
-};
-
-// Where a workgroup's positions are.
+// A workgroup's tokens, and a lane's.
 struct Place {
-  int64_t row, start, base;             // base: its first position
-  int32_t count;
-  __device__ Place(const MoveArgs& a) {
+  int64_t row, pos;                     // pos: in the cache
+  int32_t t;
+  bool asked, live;                     // among the row's tokens (reads: the call's); its position is one of the cache
+  __device__ Place(const MoveArgs& a, bool read) {
     row = blockIdx.x / (uint32_t)a.groups;
-    const int32_t group = blockIdx.x % (uint32_t)a.groups;
-    start = a.start ? a.start[row] : 0;
-    count = a.counts ? a.counts[row] : a.n;
-    count = count < 0 ? 0 : count > a.n ? a.n : count;
-    base = (start & ~(int64_t)(kGroup - 1)) + kGroup * group;
+    t = kGroup * (int32_t)(blockIdx.x % (uint32_t)a.groups) + (threadIdx.x & 63) / 8;
+    int32_t count = a.counts ? a.counts[row] : a.n;
+    count = count > a.n ? a.n : count;
+    pos = (int64_t)(a.start ? a.start[row] : 0) + t;
+    live = t < count && pos >= 0 && pos < a.held.cap;
+    asked = t < (read ? a.n : count);
   }
 };
 
-// Makes what the lanes of a wave have written to LDS visible to each other.
-__device__ inline void turn_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
-// Where the values of eight tokens of a d lie in a block's values.
-template <bool FP8>
-__device__ inline int value_place(int d, int u, int half) {
-  return (((d / 32 * 2 + u) * 2 + half) * 32 + (d & 31)) * (FP8 ? 8 : 16);
-}
-// ... and eight d's of a token's keys in a block's keys.
-template <bool FP8>
-__device__ inline int key_place(int piece, int token) {
-  return FP8 ? (((piece >> 2) * 2 + (piece & 1)) * kBlock + key_row(token)) * 16 + (piece >> 1 & 1) * 8 : (piece * kBlock + key_row(token)) * 16;
-}
+// The d's of a lane: 16 of each 128, in two pieces of eight (at most: D may be 64 or 96).
+template <int D>
+struct Pieces {
+  static constexpr int kPieces = (D + 127) / 128 * 2;
+  static __device__ int d(int x) { return x / 2 * 128 + (threadIdx.x & 7) * 16 + x % 2 * 8; }
+};
 
 // The exponent (biased) of the least power of two s with a <= 448 s = 1.75 * 2^8 s.
 __device__ inline uint32_t scale_exponent(float a) {
@@ -96,99 +76,58 @@ __device__ inline float largest(typename T::Eight x, float a) {
 template <class T, int D, bool FP8>
 __global__ __launch_bounds__(64 * kMoveWaves) void cache_write_kernel(MoveArgs a) {
   typedef typename T::Eight Eight;
-  typedef typename Cell<T, FP8>::Type One;
-  typedef typename Cell<T, FP8>::Eight Tokens;
-  constexpr int kPieces = (D / 8 + 7) / 8, kColumns = (D + 63) / 64;   // of a lane: 16-byte pieces of a token, d's of eight tokens
-  // (rows of D + 16 bytes apart: eight tokens' pieces in different banks, pieces aligned)
-  __shared__ alignas(16) One turned[kMoveWaves][kGroup][D + 16 / sizeof(One)];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Place at(a);
-  const int64_t pos = at.base + (lane >> 3), t = pos - at.start;
-  const bool asked = t >= 0 && t < at.count, live = asked && pos >= 0 && pos < a.held.cap;
-  if (wave == 0 && asked && !live) atomicOr(a.status, CSD_STATUS_CAPACITY);
-  const uint64_t lives = __ballot(live);                 // eight lanes a token
-  if (lives == 0) return;
-  // the group's place in its block (some position of it is inside, so its base is not negative)
-  const int64_t block_of = at.base / kBlock;
-  const int token = (int)(at.base & (kBlock - 1)) + (lane >> 3), u = token / 16, half = token / 8 & 1;
-  for (int32_t head0 = wave; head0 < a.Hk; head0 += kMoveWaves * kHeads) {
-    Eight k[kHeads][kPieces], v[kHeads][kPieces];
-    Tokens old[kHeads][kColumns];
+  typedef typename T::One Value;
+  typedef Pieces<D> P;
+  const int wave = threadIdx.x >> 6;
+  const Place at(a, false);
+  if (wave == 0 && at.asked && !at.live) atomicOr(a.status, CSD_STATUS_CAPACITY);
+  if (__ballot(at.live) == 0) return;
+  const int64_t block_of = at.live ? at.pos / kBlock : 0;
+  const int token = (int)at.pos & (kBlock - 1);
+  for (int32_t head = wave; head < a.Hk; head += kMoveWaves) {
+    Eight k[P::kPieces], v[P::kPieces];
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) {
-      const int32_t head = head0 + h * kMoveWaves;
-      if (head >= a.Hk) continue;
-#pragma unroll
-      for (int x = 0; x < kPieces; ++x) {
-        const int d = ((lane & 7) + 8 * x) * 8;
-        k[h][x] = v[h][x] = Eight{};
-        if (live && d < D) {
-          k[h][x] = *reinterpret_cast<const Eight*>(static_cast<const typename T::One*>(a.k.data) + at.row * a.k.row_stride + t * a.k.token_stride + head * a.k.head_stride + d);
-          v[h][x] = *reinterpret_cast<const Eight*>(static_cast<const typename T::One*>(a.v.data) + at.row * a.v.row_stride + t * a.v.token_stride + head * a.v.head_stride + d);
-        }
-      }
-      if (lives != ~0ull) {
-        const uint8_t* const values = a.held.data + (a.held.first(at.row, head, a.Hk) + block_of) * a.held.block_bytes + a.held.block_bytes / 2;
-#pragma unroll
-        for (int x = 0; x < kColumns; ++x)
-          if (lane + 64 * x < D) old[h][x] = *reinterpret_cast<const Tokens*>(values + value_place<FP8>(lane + 64 * x, u, half));
+    for (int x = 0; x < P::kPieces; ++x) {
+      k[x] = v[x] = Eight{};
+      if (at.live && P::d(x) < D) {
+        k[x] = *reinterpret_cast<const Eight*>(static_cast<const Value*>(a.k.data) + at.row * a.k.row_stride + at.t * a.k.token_stride + head * a.k.head_stride + P::d(x));
+        v[x] = *reinterpret_cast<const Eight*>(static_cast<const Value*>(a.v.data) + at.row * a.v.row_stride + at.t * a.v.token_stride + head * a.v.head_stride + P::d(x));
       }
     }
+    const int64_t block = a.held.first(at.row, head, a.Hk) + block_of, to = (block * kBlock + token) * D * (FP8 ? 1 : 2);
+    if constexpr (FP8) {
+      float k_most = 0, v_most = 0;
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) {
-      const int32_t head = head0 + h * kMoveWaves;
-      if (head >= a.Hk) continue;
-      const int64_t block = a.held.first(at.row, head, a.Hk) + block_of;
-      uint8_t* const data = a.held.data + block * a.held.block_bytes;
-      float k_down = 1.0f, v_down = 1.0f;
-      if constexpr (FP8) {
-        float k_most = 0, v_most = 0;
-#pragma unroll
-        for (int x = 0; x < kPieces; ++x) {
-          k_most = largest<T>(k[h][x], k_most);
-          v_most = largest<T>(v[h][x], v_most);
-        }
-#pragma unroll
-        for (int r = 1; r < 8; r *= 2) {
-          k_most = fmaxf(k_most, __shfl_xor(k_most, r));
-          v_most = fmaxf(v_most, __shfl_xor(v_most, r));
-        }
-        const uint32_t k_exp = scale_exponent(k_most), v_exp = scale_exponent(v_most);
-        k_down = __uint_as_float((254 - k_exp) << 23);
-        v_down = __uint_as_float((254 - v_exp) << 23);
-        if (live && (lane & 7) == 0) {
-          uint8_t* const scale = a.held.scale + block * kScaleBytes;
-          scale[key_row(token)] = (uint8_t)k_exp;
-          scale[kBlock + token] = (uint8_t)v_exp;
-        }
+      for (int x = 0; x < P::kPieces; ++x) {
+        k_most = largest<T>(k[x], k_most);
+        v_most = largest<T>(v[x], v_most);
       }
-      turn_sync();                                       // (the last head's have been read)
 #pragma unroll
-      for (int x = 0; x < kPieces; ++x) {
-        const int piece = (lane & 7) + 8 * x;
-        if (piece * 8 >= D) continue;
-        if constexpr (FP8) {
-          if (live) *reinterpret_cast<Pair*>(data + key_place<FP8>(piece, token)) = to_fp8<T>(k[h][x], k_down);
-          *reinterpret_cast<Pair*>(&turned[wave][lane >> 3][piece * 8]) = to_fp8<T>(v[h][x], v_down);
-        } else {
-          if (live) *reinterpret_cast<Eight*>(data + key_place<FP8>(piece, token)) = k[h][x];
-          *reinterpret_cast<Eight*>(&turned[wave][lane >> 3][piece * 8]) = v[h][x];
-        }
+      for (int r = 1; r < 8; r *= 2) {
+        k_most = fmaxf(k_most, __shfl_xor(k_most, r));
+        v_most = fmaxf(v_most, __shfl_xor(v_most, r));
       }
-      turn_sync();
+      const uint32_t k_exp = scale_exponent(k_most), v_exp = scale_exponent(v_most);
+      const float k_down = __uint_as_float((254 - k_exp) << 23), v_down = __uint_as_float((254 - v_exp) << 23);
+      if (!at.live) continue;
+      if ((threadIdx.x & 7) == 0) {
+        uint8_t* const scale = a.held.scale + block * kScaleBytes;
+        scale[token] = (uint8_t)k_exp;
+        scale[kBlock + token] = (uint8_t)v_exp;
+      }
 #pragma unroll
-      for (int x = 0; x < kColumns; ++x) {
-        const int d = lane + 64 * x;
-        if (d >= D) continue;
-        union {
-          One one[kGroup];
-          Tokens all;
-        } y;
-        if (lives != ~0ull) y.all = old[h][x];
+      for (int x = 0; x < P::kPieces; x += 2) {
+        if (P::d(x) >= D) continue;
+        const Pair k0 = to_fp8<T>(k[x], k_down), k1 = to_fp8<T>(k[x + 1], k_down), v0 = to_fp8<T>(v[x], v_down), v1 = to_fp8<T>(v[x + 1], v_down);
+        *reinterpret_cast<Words*>(a.held.keys + to + P::d(x)) = Words{k0[0], k0[1], k1[0], k1[1]};
+        *reinterpret_cast<Words*>(a.held.values + to + P::d(x)) = Words{v0[0], v0[1], v1[0], v1[1]};
+      }
+    } else if (at.live) {
 #pragma unroll
-        for (int i = 0; i < kGroup; ++i)
-          if (lives >> (8 * i) & 1) y.one[i] = turned[wave][i][d];
-        *reinterpret_cast<Tokens*>(data + a.held.block_bytes / 2 + value_place<FP8>(d, u, half)) = y.all;
+      for (int x = 0; x < P::kPieces; ++x) {
+        if (P::d(x) >= D) continue;
+        *reinterpret_cast<Eight*>(a.held.keys + to + P::d(x) * 2) = k[x];
+        *reinterpret_cast<Eight*>(a.held.values + to + P::d(x) * 2) = v[x];
       }
     }
   }
@@ -198,84 +137,40 @@ template <class T, int D, bool FP8>
 __global__ __launch_bounds__(64 * kMoveWaves) void cache_read_kernel(MoveArgs a) {
   typedef typename T::Eight Eight;
   typedef typename T::One Value;
-  typedef typename Cell<T, FP8>::Type One;
-  typedef typename Cell<T, FP8>::Eight Tokens;
-  constexpr int kPieces = (D / 8 + 7) / 8, kColumns = (D + 63) / 64;
-  __shared__ alignas(16) One turned[kMoveWaves][kGroup][D + 16 / sizeof(One)];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Place at(a);
-  const int64_t pos = at.base + (lane >> 3), t = pos - at.start;
-  const bool asked = t >= 0 && t < a.n;                  // written, be it with zeros
-  const bool live = asked && t < at.count && pos >= 0 && pos < a.held.cap;
-  const bool any = __ballot(live) != 0;
-  if (__ballot(asked) == 0) return;
-  // (a group of the capacity's last block may pass the capacity, never the block)
-  const int64_t block_of = any ? at.base / kBlock : 0;
-  const int token = (int)(at.base & (kBlock - 1)) + (lane >> 3), u = token / 16, half = token / 8 & 1;
-  for (int32_t head0 = wave; head0 < a.Hk; head0 += kMoveWaves * kHeads) {
-    Tokens columns[kHeads][kColumns];
-    Pair codes[kHeads][kPieces];
-    Eight k[kHeads][kPieces];
-    uint32_t k_exp[kHeads], v_exp[kHeads];
+  typedef Pieces<D> P;
+  const int wave = threadIdx.x >> 6;
+  const Place at(a, true);
+  if (!at.asked) return;
+  const int64_t block_of = at.live ? at.pos / kBlock : 0;
+  const int token = (int)at.pos & (kBlock - 1);
+  for (int32_t head = wave; head < a.Hk; head += kMoveWaves) {
+    Eight k[P::kPieces], v[P::kPieces];
+    const int64_t block = a.held.first(at.row, head, a.Hk) + block_of, from = (block * kBlock + token) * D * (FP8 ? 1 : 2);
+    float k_scale = 1.0f, v_scale = 1.0f;
+    if (FP8 && at.live) {
+      const uint8_t* const scale = a.held.scale + block * kScaleBytes;
+      k_scale = __uint_as_float((uint32_t)scale[token] << 23);
+      v_scale = __uint_as_float((uint32_t)scale[kBlock + token] << 23);
+    }
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) {
-      const int32_t head = head0 + h * kMoveWaves;
-      if (head >= a.Hk || !any) continue;
-      const int64_t block = a.held.first(at.row, head, a.Hk) + block_of;
-      const uint8_t* const data = a.held.data + block * a.held.block_bytes;
-#pragma unroll
-      for (int x = 0; x < kColumns; ++x)
-        if (lane + 64 * x < D) columns[h][x] = *reinterpret_cast<const Tokens*>(data + a.held.block_bytes / 2 + value_place<FP8>(lane + 64 * x, u, half));
-#pragma unroll
-      for (int x = 0; x < kPieces; ++x) {
-        const int piece = (lane & 7) + 8 * x;
-        if (piece * 8 >= D || !live) continue;
-        if constexpr (FP8) codes[h][x] = *reinterpret_cast<const Pair*>(data + key_place<FP8>(piece, token));
-        else k[h][x] = *reinterpret_cast<const Eight*>(data + key_place<FP8>(piece, token));
-      }
-      if (FP8 && live) {
-        const uint8_t* const scale = a.held.scale + block * kScaleBytes;
-        k_exp[h] = scale[key_row(token)];
-        v_exp[h] = scale[kBlock + token];
+    for (int x = 0; x < P::kPieces; x += FP8 ? 2 : 1) {
+      k[x] = v[x] = Eight{};
+      if constexpr (FP8) k[x + 1] = v[x + 1] = Eight{};
+      if (!at.live || P::d(x) >= D) continue;
+      if constexpr (FP8) {
+        const Words y = *reinterpret_cast<const Words*>(a.held.keys + from + P::d(x)), z = *reinterpret_cast<const Words*>(a.held.values + from + P::d(x));
+        k[x] = from_fp8<T>(Pair{y[0], y[1]}, k_scale), k[x + 1] = from_fp8<T>(Pair{y[2], y[3]}, k_scale);
+        v[x] = from_fp8<T>(Pair{z[0], z[1]}, v_scale), v[x + 1] = from_fp8<T>(Pair{z[2], z[3]}, v_scale);
+      } else {
+        k[x] = *reinterpret_cast<const Eight*>(a.held.keys + from + P::d(x) * 2);
+        v[x] = *reinterpret_cast<const Eight*>(a.held.values + from + P::d(x) * 2);
       }
     }
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) {
-      const int32_t head = head0 + h * kMoveWaves;
-      if (head >= a.Hk) continue;
-      turn_sync();                                       // (the last head's have been read)
-      if (any) {
-#pragma unroll
-        for (int x = 0; x < kColumns; ++x) {
-          union {
-            One one[kGroup];
-            Tokens all;
-          } y;
-          y.all = columns[h][x];
-          if (lane + 64 * x < D) {
-#pragma unroll
-            for (int i = 0; i < kGroup; ++i) turned[wave][i][lane + 64 * x] = y.one[i];
-          }
-        }
-      }
-      turn_sync();
-#pragma unroll
-      for (int x = 0; x < kPieces; ++x) {
-        const int piece = (lane & 7) + 8 * x, d = piece * 8;
-        if (d >= D || !asked) continue;
-        Eight key{}, value{};
-        if (live) {
-          if constexpr (FP8) {
-            key = from_fp8<T>(codes[h][x], __uint_as_float(k_exp[h] << 23));
-            value = from_fp8<T>(*reinterpret_cast<const Pair*>(&turned[wave][lane >> 3][d]), __uint_as_float(v_exp[h] << 23));
-          } else {
-            key = k[h][x];
-            value = *reinterpret_cast<const Eight*>(&turned[wave][lane >> 3][d]);
-          }
-        }
-        *reinterpret_cast<Eight*>(static_cast<Value*>(const_cast<void*>(a.k.data)) + at.row * a.k.row_stride + t * a.k.token_stride + head * a.k.head_stride + d) = key;
-        *reinterpret_cast<Eight*>(static_cast<Value*>(const_cast<void*>(a.v.data)) + at.row * a.v.row_stride + t * a.v.token_stride + head * a.v.head_stride + d) = value;
-      }
+    for (int x = 0; x < P::kPieces; ++x) {
+      if (P::d(x) >= D) continue;
+      *reinterpret_cast<Eight*>(static_cast<Value*>(const_cast<void*>(a.k.data)) + at.row * a.k.row_stride + at.t * a.k.token_stride + head * a.k.head_stride + P::d(x)) = k[x];
+      *reinterpret_cast<Eight*>(static_cast<Value*>(const_cast<void*>(a.v.data)) + at.row * a.v.row_stride + at.t * a.v.token_stride + head * a.v.head_stride + P::d(x)) = v[x];
     }
   }
 }
@@ -292,13 +187,15 @@ void of_dim(int32_t head_dim, F f) {
 
 template <bool READ>
 void cache_move(const MoveArgs& a, int32_t head_dim, bool f16, bool fp8, hipStream_t st) {
-  // as many rows a launch as keep its threads below 2^32 (a row's groups are 2^21 and a few at most)
-  const int64_t most = ((int64_t)1 << 23) / a.groups;
+  // as many rows a launch as keep its threads below 2^32 (a row's groups are 2^21 at most)
+  const int64_t most = ((int64_t)1 << 22) / a.groups;
   for (int64_t r = 0; r < a.rows; r += most) {
     MoveArgs b = a;
     b.rows = a.rows - r < most ? a.rows - r : most;
-    b.held.data += b.held.first(r, 0, a.Hk) * b.held.block_bytes;
-    if (fp8) b.held.scale += b.held.first(r, 0, a.Hk) * kScaleBytes;
+    const int64_t before = b.held.first(r, 0, a.Hk);
+    b.held.keys += before * block_bytes(head_dim, fp8);
+    b.held.values += before * block_bytes(head_dim, fp8);
+    if (fp8) b.held.scale += before * kScaleBytes;
     if (a.start) b.start += r;
     if (a.counts) b.counts += r;
     b.k.data = static_cast<const uint16_t*>(a.k.data) + r * a.k.row_stride;
