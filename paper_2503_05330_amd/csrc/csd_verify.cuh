@@ -24,6 +24,7 @@ constexpr int kScaleBytes = 2 * kBlock; // of a block's scales
 typedef float Acc __attribute__((ext_vector_type(16)));
 typedef uint32_t Words __attribute__((ext_vector_type(4)));   // 16 bytes
 typedef uint32_t Pair __attribute__((ext_vector_type(2)));
+typedef int16_t Codes __attribute__((ext_vector_type(2)));    // four of 8 bits
 
 struct BF16 {
   typedef __bf16 One;
@@ -35,6 +36,12 @@ struct BF16 {
   static __device__ Two from_fp8(uint32_t codes, float scale) {
     return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, HIGH);
   }
+  // the codes of four values over scale, a power of two
+  static __device__ uint32_t to_fp8(Two low, Two high, float scale) {
+    Codes codes{};
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(codes, low, scale, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(codes, high, scale, true));
+  }
 };
 struct F16 {
   typedef _Float16 One;
@@ -45,6 +52,12 @@ struct F16 {
   template <bool HIGH>
   static __device__ Two from_fp8(uint32_t codes, float scale) {
     return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, HIGH);
+  }
+  // the codes of four values over scale, a power of two
+  static __device__ uint32_t to_fp8(Two low, Two high, float scale) {
+    Codes codes{};
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(codes, low, scale, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(codes, high, scale, true));
   }
 };
 

@@ -3,8 +3,10 @@
 // A workgroup takes eight tokens of one row, its waves the kv heads, which lie side by side in a projection's output.  Eight
 // lanes hold a token, so that its largest value is found in three exchanges; a lane has 16 values of each 128 of a token,
 // 16 bytes of codes.  Long calls are bound by the copy: 8 prompts of up to 4096 tokens (half of them there), 8 heads of 128, are written
-// to 8 bits in 23.9 us and read back, with zeros for the missing, in 35.9: 4.2 and 4.7 TB/s.  Short ones are bound by the launch
-// and the loads before a row's place is known: 64 x 16 paths of up to 9 tokens, 8 heads of 128, take 15.5 us to 8 bits.
+// to 8 bits in 22.4 us and read back, with zeros for the missing, in 36.1: 4.5 and 4.7 TB/s.  Short ones are bound by the launch
+// and the loads before a row's place is known: 64 x 16 paths of up to 9 tokens, 8 heads of 128, take 10.1 us to 8 bits (15.5 where
+// maxima and codes are taken in 32 bits; the type's own comparisons and conversion do two values an instruction, and exactly
+// that while all are finite).
 #include "csd_verify.cuh"
 
 namespace csd {
@@ -45,32 +47,68 @@ __device__ inline uint32_t scale_exponent(float a) {
   return e < 1 ? 1 : (uint32_t)e;
 }
 
-// Eight values quantised; `down` is 1 / s.
-template <class T>
-__device__ inline Pair to_fp8(typename T::Eight x, float down) {
+// Eight values quantised by a power of two, each rounded once, to nearest; SOME_ODD: there may be infinities, which become the
+// largest code.
+template <class T, bool SOME_ODD>
+__device__ inline Pair to_fp8(typename T::Eight x, float scale) {
   Pair codes;
+  if constexpr (SOME_ODD) {
+    const float down = __uint_as_float((254u << 23) - __float_as_uint(scale));   // 1 / scale
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    float y[4];
+    for (int w = 0; w < 2; ++w) {
+      float y[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      y[i] = (float)x[4 * w + i] * down;                              // exact
-      y[i] = fabsf(y[i]) > 448.0f ? copysignf(448.0f, y[i]) : y[i];   // an infinity; NaN stays
+      for (int i = 0; i < 4; ++i) {
+        y[i] = (float)x[4 * w + i] * down;                              // exact
+        y[i] = fabsf(y[i]) > 448.0f ? copysignf(448.0f, y[i]) : y[i];   // an infinity; NaN stays
+      }
+      const int code = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+      codes[w] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], code, true);
     }
-    int code = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    codes[w] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], code, true);
+  } else {
+    union {
+      typename T::Eight eight;
+      typename T::Two two[4];
+    } y{x};
+    codes[0] = T::to_fp8(y.two[0], y.two[1], scale);
+    codes[1] = T::to_fp8(y.two[2], y.two[3], scale);
   }
   return codes;
 }
 
-template <class T>
-__device__ inline float largest(typename T::Eight x, float a) {
+// The bits of the largest magnitude of a lane's pieces, infinity and NaN among them (they order as the values do) ...
+template <class T, int N>
+__device__ inline uint32_t largest_bits(const typename T::Eight (&x)[N]) {
+  typedef uint16_t __attribute__((ext_vector_type(2))) Halves;
+  Halves most{};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = fabsf((float)x[i]);
-    a = y < INFINITY && y > a ? y : a;                                // finite ones alone
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) most = __builtin_elementwise_max(most, __builtin_bit_cast(Halves, __builtin_bit_cast(Words, x[i])[w] & 0x7fff7fffu));
+  return most[0] > most[1] ? most[0] : most[1];
+}
+// ... and the largest finite one.
+template <class T, int N>
+__device__ inline float largest_finite(const typename T::Eight (&x)[N]) {
+  float most = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float y = fabsf((float)x[i][e]);
+      most = y < INFINITY && y > most ? y : most;
+    }
+  return most;
+}
+// of the eight lanes of a token
+template <class X>
+__device__ inline X over_token(X x) {
+#pragma unroll
+  for (int r = 1; r < 8; r *= 2) {
+    const X y = __shfl_xor(x, r);
+    x = y > x ? y : x;
   }
-  return a;
+  return x;
 }
 
 template <class T, int D, bool FP8>
@@ -96,32 +134,34 @@ __global__ __launch_bounds__(64 * kMoveWaves) void cache_write_kernel(MoveArgs a
     }
     const int64_t block = a.held.first(at.row, head, a.Hk) + block_of, to = (block * kBlock + token) * D * (FP8 ? 1 : 2);
     if constexpr (FP8) {
-      float k_most = 0, v_most = 0;
-#pragma unroll
-      for (int x = 0; x < P::kPieces; ++x) {
-        k_most = largest<T>(k[x], k_most);
-        v_most = largest<T>(v[x], v_most);
-      }
-#pragma unroll
-      for (int r = 1; r < 8; r *= 2) {
-        k_most = fmaxf(k_most, __shfl_xor(k_most, r));
-        v_most = fmaxf(v_most, __shfl_xor(v_most, r));
+      const uint32_t k_bits = over_token(largest_bits<T>(k)), v_bits = over_token(largest_bits<T>(v));
+      const bool odd = __ballot(k_bits >= T::kExponent || v_bits >= T::kExponent) != 0;
+      float k_most = (float)__builtin_bit_cast(Value, (uint16_t)k_bits), v_most = (float)__builtin_bit_cast(Value, (uint16_t)v_bits);
+      if (odd) {
+        k_most = over_token(largest_finite<T>(k));
+        v_most = over_token(largest_finite<T>(v));
       }
       const uint32_t k_exp = scale_exponent(k_most), v_exp = scale_exponent(v_most);
-      const float k_down = __uint_as_float((254 - k_exp) << 23), v_down = __uint_as_float((254 - v_exp) << 23);
+      const float k_scale = __uint_as_float(k_exp << 23), v_scale = __uint_as_float(v_exp << 23);
       if (!at.live) continue;
       if ((threadIdx.x & 7) == 0) {
         uint8_t* const scale = a.held.scale + block * kScaleBytes;
         scale[token] = (uint8_t)k_exp;
         scale[kBlock + token] = (uint8_t)v_exp;
       }
+      const auto store = [&](auto some_odd) {
+        constexpr bool kOdd = some_odd();
 #pragma unroll
-      for (int x = 0; x < P::kPieces; x += 2) {
-        if (P::d(x) >= D) continue;
-        const Pair k0 = to_fp8<T>(k[x], k_down), k1 = to_fp8<T>(k[x + 1], k_down), v0 = to_fp8<T>(v[x], v_down), v1 = to_fp8<T>(v[x + 1], v_down);
-        *reinterpret_cast<Words*>(a.held.keys + to + P::d(x)) = Words{k0[0], k0[1], k1[0], k1[1]};
-        *reinterpret_cast<Words*>(a.held.values + to + P::d(x)) = Words{v0[0], v0[1], v1[0], v1[1]};
-      }
+        for (int x = 0; x < P::kPieces; x += 2) {
+          if (P::d(x) >= D) continue;
+          const Pair k0 = to_fp8<T, kOdd>(k[x], k_scale), k1 = to_fp8<T, kOdd>(k[x + 1], k_scale);
+          const Pair v0 = to_fp8<T, kOdd>(v[x], v_scale), v1 = to_fp8<T, kOdd>(v[x + 1], v_scale);
+          *reinterpret_cast<Words*>(a.held.keys + to + P::d(x)) = Words{k0[0], k0[1], k1[0], k1[1]};
+          *reinterpret_cast<Words*>(a.held.values + to + P::d(x)) = Words{v0[0], v0[1], v1[0], v1[1]};
+        }
+      };
+      if (odd) store(std::true_type{});
+      else store(std::false_type{});
     } else if (at.live) {
 #pragma unroll
       for (int x = 0; x < P::kPieces; ++x) {

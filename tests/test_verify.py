@@ -124,6 +124,25 @@ def test_eight_bit_codes_of_special_values(dtype):
     assert same(k, held(x, True).to(dtype)) and same(v, held(x.flip(-1), True).to(dtype))
 
 
+@pytest.mark.parametrize("dtype,least,most", [(BF, -133, 127), (F16, -24, 15)])
+@pytest.mark.parametrize("odd", [False, True])
+def test_eight_bit_codes_at_every_size(gen, dtype, least, most, odd):
+    """Tokens of every magnitude of the type, subnormal ones among them, each rounded once to what its scale allows; a token
+    with an infinity beside them changes nothing."""
+    D = 128
+    sizes = 2.0 ** torch.arange(least, most + 1, device="cuda", dtype=torch.float64)
+    x = torch.rand((len(sizes), D), generator=gen, device="cuda", dtype=torch.float64) * sizes[:, None]
+    x = (x * torch.sign(torch.randn(x.shape, generator=gen, device="cuda", dtype=torch.float64))).to(dtype)
+    x[:, :D // 4] *= 2.0 ** -9                           # the codes' own subnormal numbers
+    if odd:
+        x[::8, 5] = float("inf")
+    c = verify.PathCache(1, 1, 0, len(x), 1, 1, D, 1, dtype=dtype, fp8=True)
+    c.write(0, x[None, None, :, None], x.flip(-1)[None, None, :, None])
+    k, v = c.read(0, len(x))
+    want = held(x, True).to(dtype)
+    assert same(k[0, 0, :, 0], want) and same(v[0, 0, :, 0], want.flip(-1))
+
+
 @pytest.mark.parametrize("prompt", [False, True])
 def test_positions_outside_of_the_cache_are_dropped_and_reported(gen, prompt):
     P, N, cap, H, D = 2, 2, 40, 2, 64
