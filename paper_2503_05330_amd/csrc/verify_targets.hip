@@ -170,10 +170,10 @@ __global__ __launch_bounds__(64) void targets_join_kernel(TargetArgs a) {
 // least (us in one launch / in two: 8 rows of 152064 20.9 / 7.9, 64 22.5 / 12.9, 128 22.8 / 17.3, 8 of 50257 9.8 / 7.7; but 4
 // rows of 32000 7.8 / 7.4, which the second launch costs a caller, and 2 of 16000 5.9 / 6.9).  Many rows of more than half a megabyte, logits and noise, are cut in
 // eight, so that the last ones leave no CU idle (1088 rows of 152064 with noise 182 / 165, 768 126 / 119; 768 without
-// noise 52 / 63).
-constexpr int32_t kMostParts = 32, kLeastLogits = 2048, kLongParts = 8;
+// noise 52 / 63); so many that a launch would have more than 2^31 threads are not.
+constexpr int32_t kMostParts = 32, kLeastLogits = 2048, kLongParts = 8, kThreads = 512;
 int32_t parts_of(int64_t rows, int32_t vocab, int64_t bytes) {
-  if (rows >= 512) return bytes * vocab >= 1 << 19 ? kLongParts : 1;
+  if (rows >= 512) return bytes * vocab >= 1 << 19 && rows * kLongParts * kThreads <= (int64_t)1 << 31 ? kLongParts : 1;
   int64_t parts = 256 * (int64_t)vocab / 100000 / rows;
   if (parts > vocab / kLeastLogits) parts = vocab / kLeastLogits;
   return vocab < 40000 || parts < 1 ? 1 : parts > kMostParts ? kMostParts : (int32_t)parts;
@@ -181,7 +181,7 @@ int32_t parts_of(int64_t rows, int32_t vocab, int64_t bytes) {
 
 template <class E, bool NOISE>
 void targets(const TargetArgs& a, hipStream_t st) {
-  targets_kernel<E, NOISE, 512><<<(uint32_t)(a.rows * a.parts), 512, 0, st>>>(a);
+  targets_kernel<E, NOISE, kThreads><<<(uint32_t)(a.rows * a.parts), kThreads, 0, st>>>(a);
   if (a.parts > 1) targets_join_kernel<<<(uint32_t)a.rows, 64, 0, st>>>(a);
 }
 

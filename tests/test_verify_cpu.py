@@ -99,6 +99,13 @@ def test_null_and_misaligned_arguments_are_refused(lib):
         assert targets(**bad) == b.ERR_INVALID_ARG, bad
 
 
+def test_rows_of_targets_share_a_launch_of_less_than_two_to_the_32_threads(lib):
+    size = ctypes.c_size_t()
+    for rows in (1 << 19, (1 << 19) + 1, 1 << 20, 1 << 22):                # (a scratch: eight workgroups of 512 threads a row)
+        assert lib.csd_targets_bytes(rows, 152064, ctypes.byref(size)) == 0
+        assert (rows * 8 * 512 < 1 << 32) if size.value else (rows * 512 < 1 << 32)
+
+
 def test_tensors_of_the_host_are_refused(lib):
     import torch
     with pytest.raises(TypeError):
