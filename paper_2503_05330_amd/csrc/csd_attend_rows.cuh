@@ -280,9 +280,9 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // the item
-  const bool prompt = (int32_t)blockIdx.x < a.prompt_groups;
+  uint32_t item = a.paths_first ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+  const bool prompt = (int32_t)item < a.prompt_groups;
   const bool solo = !prompt && a.solo, results = a.how == kDirect;
-  uint32_t item = blockIdx.x;
   if (!prompt) item -= a.prompt_groups;
   if (solo) item = item * kWaves + wave;
   // `inner` items that have tokens in common lie behind each other, or, as workgroups are dealt to the eight XCDs in turn, eight

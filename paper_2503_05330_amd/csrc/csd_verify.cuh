@@ -102,6 +102,7 @@ struct AttendArgs {
   int32_t prompt_tiles, path_tiles;  // tiles of query rows of a (problem, kv head), of a (path, kv head)
   int32_t prompt_groups;             // workgroups of the prompts' items, before those of the paths'
   int32_t solo;                      // a path's item is one wave's instead of a workgroup's
+  int32_t paths_first;               // the items in the reverse order
   int32_t prompt_turns, path_turns;  // whether items that have tokens in common go to one XCD
   int32_t how;                       // one of these
 };

@@ -18,16 +18,16 @@ void attend_dim(const AttendArgs& a, const AttendLaunch& how, int32_t head_dim, 
 
 struct Shape {
   int32_t how;
-  bool solo;
+  bool solo, paths_first;
   int64_t prompt_tiles, path_tiles, prompt_splits, path_splits;
 };
 
 // The forms of a launch, and what each takes, ns, as far as the sizes tell: a start, the blocks that a wave goes through one after
 // the other, all blocks and all workgroups over what the chip holds of them (two workgroups a CU), and the parts that are written
 // and read again.  Fits of the measured times of 460 draws of 1 .. 64 problems of 1 .. 64 paths, 1 .. 17 tokens, prompts of 1 .. 8192
-// and paths of 2 .. 4100 tokens, heads of 64 and 128; each fit misses by 18 .. 20 %.  The form with the smallest is 2.6 % slower than
-// the fastest of 13 (parts split for 256, 512 or 1024 workgroups and 4, 8 or 16 blocks at least; geometric mean, 1.37
-// times at worst).  The best of one form for all sizes is 22 % slower: one launch with the whole prompt for each path.
+// and paths of 2 .. 4100 tokens, heads of 64 and 128; each fit misses by 18 .. 20 %.  Over 800 other draws the form with the smallest is
+// 2.6 % slower than the fastest of 13 (parts split for 256, 512 or 1024 workgroups and 4, 8 or 16 blocks at least; geometric
+// mean, 1.40 times at worst).  The best of one form for all sizes is 23 % slower: the prompt's parts apart, a wave an item.
 struct Cost {
   int64_t start, round, blocks, groups, parts;
   int64_t operator()(double rounds, double all_blocks, double all_groups, double part_values) const {
@@ -41,13 +41,13 @@ Shape shape_of(int64_t problems, int64_t N, int64_t rows, int64_t head_dim, int6
   auto groups_of = [](int64_t x) { return x <= 32 ? 1 : x <= 64 ? 2 : 4; };             // of 32 rows in a tile of 128
   const int64_t tiles = over(rows, 128), solo_tiles = over(rows, 32);
   const double share = groups_of(rows) / 4.0;                                            // of a workgroup that has a block
-  Shape best{kDirect, false, 0, tiles, 0, 1};
+  Shape best{kDirect, false, false, 0, tiles, 0, 1};
   int64_t least = Cost{8400, 470, 800, 4900, 0}(both * share, (double)paths * tiles * both * share, (double)paths * tiles, 0);
   auto offer = [&](const Shape& s, int64_t cost) {
     if (cost < least) best = s, least = cost;
   };
   // a wave an item
-  offer(Shape{kDirect, true, 0, solo_tiles, 0, 1},
+  offer(Shape{kDirect, true, false, 0, solo_tiles, 0, 1},
         Cost{8300, 530, 840, 6300, 0}(both, (double)paths * solo_tiles * both / 4, (double)paths * solo_tiles / 4, 0));
   // the prompt's part for all paths together
   for (const bool solo : {false, true}) {
@@ -63,7 +63,10 @@ Shape shape_of(int64_t problems, int64_t N, int64_t rows, int64_t head_dim, int6
     const double groups = (double)problems * prompt_tiles * s + (double)paths * path_tiles * t / (solo ? 4 : 1);
     const double values = (double)paths * rows * (s + t) * head_dim;
     const Cost cost = solo ? Cost{11400, 590, 640, 6700, 860} : Cost{11600, 410, 650, 7200, 420};
-    offer(Shape{kParts, solo, prompt_tiles, path_tiles, s, t}, cost(prompt_rounds > path_rounds ? prompt_rounds : path_rounds, all, groups, values));
+    // (the longer items first, so that short ones are left for the end: 64 paths x 17 tokens of 4096 + 4096, which go through 43 and 64 blocks,
+    // 115 / 109 us; the others' prompts are first, 64 problems x 16 x 1 of 4096 + 512 240 / 254 us)
+    const bool paths_first = path_rounds > prompt_rounds;
+    offer(Shape{kParts, solo, paths_first, prompt_tiles, path_tiles, s, t}, cost(prompt_rounds > path_rounds ? prompt_rounds : path_rounds, all, groups, values));
   }
   return best;
 }
@@ -76,6 +79,7 @@ void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound,
   const Shape shape = shape_of(problems, a.N, a.n * a.G, cfg.head_dim, prompt_blocks, path_blocks);
   a.how = shape.how;
   a.solo = shape.solo;
+  a.paths_first = shape.paths_first;
   a.prompt_tiles = (int32_t)shape.prompt_tiles;
   a.path_tiles = (int32_t)shape.path_tiles;
   a.prompt_splits = (int32_t)shape.prompt_splits;
