@@ -17,6 +17,9 @@ namespace csd {
 namespace verify {
 
 constexpr int kWaves = 4, kWide = 32 * kWaves;
+// While there are both, workgroups take as many items of paths as there are CUs, then of prompts, in turn: a CU with one of each loads for the
+// one while it computes for the other (64 paths x 17 tokens of 4096 + 4096: 120 us in order, 115 so, 121 in turns of 8).
+constexpr uint32_t kDeal = 256;
 
 template <class T>
 __device__ inline void store8(void* out, int64_t at, const float (&x)[8]) {
@@ -280,8 +283,18 @@ __global__ __launch_bounds__(64 * kWaves, (Ring<D, FP8>::kResident)) void attend
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // the item
-  uint32_t item = a.paths_first ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
-  const bool prompt = (int32_t)item < a.prompt_groups;
+  const uint32_t prompts = a.prompt_groups, paths = gridDim.x - prompts, dealt = (prompts < paths ? prompts : paths) / kDeal * kDeal;
+  uint32_t item = blockIdx.x;                            // the prompts' items, then the paths'
+  if (item < 2 * dealt) {
+    const uint32_t deal = item / kDeal;
+    item = deal / 2 * kDeal + item % kDeal + (deal % 2 ? 0 : prompts);
+  } else if (a.paths_first) {
+    item -= dealt;                                       // (of the paths')
+    item = item < paths ? prompts + item : item - paths + dealt;
+  } else if (item < prompts + dealt) {
+    item -= dealt;
+  }
+  const bool prompt = item < prompts;
   const bool solo = !prompt && a.solo, results = a.how == kDirect;
   if (!prompt) item -= a.prompt_groups;
   if (solo) item = item * kWaves + wave;

@@ -102,7 +102,7 @@ struct AttendArgs {
   int32_t prompt_tiles, path_tiles;  // tiles of query rows of a (problem, kv head), of a (path, kv head)
   int32_t prompt_groups;             // workgroups of the prompts' items, before those of the paths'
   int32_t solo;                      // a path's item is one wave's instead of a workgroup's
-  int32_t paths_first;               // the items in the reverse order
+  int32_t paths_first;               // before the prompts'
   int32_t prompt_turns, path_turns;  // whether items that have tokens in common go to one XCD
   int32_t how;                       // one of these
 };
@@ -131,8 +131,10 @@ void attend_96(const AttendArgs& a, const AttendLaunch& how, hipStream_t st);
 void attend_128(const AttendArgs& a, const AttendLaunch& how, hipStream_t st);
 void attend_256(const AttendArgs& a, const AttendLaunch& how, hipStream_t st);
 
-// The bounds are of the lengths, parts: how many parts of rows a call may write.
-void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound, int32_t path_bound, int64_t parts, hipStream_t st);
+// The bounds are of the lengths.
+void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound, int32_t path_bound, hipStream_t st);
+// How many parts calls of so many rows write at most.
+int64_t parts_of_rows(int64_t rows, int32_t prompt_cap, int32_t path_cap);
 void cache_write(const MoveArgs& a, int32_t head_dim, bool f16, bool fp8, hipStream_t st);
 void cache_read(const MoveArgs& a, int32_t head_dim, bool f16, bool fp8, hipStream_t st);
 

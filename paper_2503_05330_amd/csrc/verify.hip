@@ -13,14 +13,9 @@ namespace {
 constexpr int64_t kWorkspaceAlign = 256;
 int64_t aligned_up(int64_t x) { return (x + kWorkspaceAlign - 1) / kWorkspaceAlign * kWorkspaceAlign; }
 
-// Parts of rows that a call may write: two for each row of the largest call (the prompt's and the path's), or enough more to
-// split the axes of a call of few rows.
-constexpr int64_t kMoreParts = 1 << 16;
-
 struct CacheLayout {
   int64_t prompt_keys, prompt_values, path_keys, path_values, prompt_scale, path_scale, part_o, part_lse, status, total;
   int64_t prompt_layer, path_layer;      // blocks of a layer
-  int64_t parts;
 };
 
 int check(const csd_cache_config* c) {
@@ -46,7 +41,7 @@ bool layout_of(const csd_cache_config* c, CacheLayout* l) {
   l->prompt_layer = (int64_t)c->n_problems * c->n_kv_heads * ((c->prompt_cap + kBlock - 1) / kBlock);
   l->path_layer = (int64_t)c->n_problems * c->n_paths * c->n_kv_heads * ((c->path_cap + kBlock - 1) / kBlock);
   const int64_t rows = (int64_t)c->n_problems * c->n_paths * c->max_step * c->n_heads;
-  l->parts = 2 * rows + kMoreParts;
+  const int64_t parts = parts_of_rows(rows, c->prompt_cap, c->path_cap);
   int64_t at = 0;
   auto take = [&](int64_t* place, int64_t size) {
     *place = at;
@@ -58,8 +53,8 @@ bool layout_of(const csd_cache_config* c, CacheLayout* l) {
   take(&l->path_values, c->n_layers * l->path_layer * per_block);
   take(&l->prompt_scale, c->fp8 ? c->n_layers * l->prompt_layer * kScaleBytes : 0);
   take(&l->path_scale, c->fp8 ? c->n_layers * l->path_layer * kScaleBytes : 0);
-  take(&l->part_o, l->parts * c->head_dim * 4);
-  take(&l->part_lse, l->parts * 4);
+  take(&l->part_o, parts * c->head_dim * 4);
+  take(&l->part_lse, parts * 4);
   take(&l->status, 4);
   l->total = at;
   return true;
@@ -226,7 +221,7 @@ int csd_attend(csd_cache* cache, int32_t layer, const csd_heads* q, const int32_
   a.rows = (int64_t)a.P * a.N * n * a.H;
   if (prompt_bound == 0 || prompt_bound > cfg.prompt_cap) prompt_bound = cfg.prompt_cap;
   if (path_bound == 0 || path_bound > cfg.path_cap) path_bound = cfg.path_cap;
-  attend_any(a, cfg, prompt_bound, path_bound, cache->layout.parts, static_cast<hipStream_t>(stream));
+  attend_any(a, cfg, prompt_bound, path_bound, static_cast<hipStream_t>(stream));
   return finish("csd_attend");
 }
 

@@ -16,6 +16,9 @@ void attend_dim(const AttendArgs& a, const AttendLaunch& how, int32_t head_dim, 
   }
 }
 
+// Items that parts are split for, and the blocks that a part has at least.
+constexpr int64_t kItems = 512, kLeastBlocks = 8;
+
 struct Shape {
   int32_t how;
   bool solo, paths_first;
@@ -25,9 +28,9 @@ struct Shape {
 // The forms of a launch, and what each takes, ns, as far as the sizes tell: a start, the blocks that a wave goes through one after
 // the other, all blocks and all workgroups over what the chip holds of them (two workgroups a CU), and the parts that are written
 // and read again.  Fits of the measured times of 460 draws of 1 .. 64 problems of 1 .. 64 paths, 1 .. 17 tokens, prompts of 1 .. 8192
-// and paths of 2 .. 4100 tokens, heads of 64 and 128; each fit misses by 18 .. 20 %.  Over 800 other draws the form with the smallest is
-// 2.6 % slower than the fastest of 13 (parts split for 256, 512 or 1024 workgroups and 4, 8 or 16 blocks at least; geometric
-// mean, 1.40 times at worst).  The best of one form for all sizes is 23 % slower: the prompt's parts apart, a wave an item.
+// and paths of 2 .. 4100 tokens, heads of 64 and 128; each fit misses by 18 .. 20 %.  Over 1200 other draws the form with the smallest is
+// 2.5 % slower than the fastest of 13 (parts split for 256, 512 or 1024 workgroups and 4, 8 or 16 blocks at least; geometric
+// mean, 1.35 times at worst).  The best of one form for all sizes is 23 % slower: one launch with the whole prompt for each path.
 struct Cost {
   int64_t start, round, blocks, groups, parts;
   int64_t operator()(double rounds, double all_blocks, double all_groups, double part_values) const {
@@ -53,7 +56,7 @@ Shape shape_of(int64_t problems, int64_t N, int64_t rows, int64_t head_dim, int6
   for (const bool solo : {false, true}) {
     const int64_t path_tiles = solo ? solo_tiles : tiles, prompt_tiles = over(N * rows, 128);
     auto splits = [&](int64_t blocks, int64_t items) {
-      const int64_t most = over(blocks, solo ? 8 : 16), x = over(512, items);
+      const int64_t most = over(blocks, solo ? kLeastBlocks : 2 * kLeastBlocks), x = over(kItems, items);
       return x < most ? x : most;
     };
     const int64_t s = prompt_blocks ? splits(prompt_blocks, problems * prompt_tiles) : 0, t = splits(path_blocks, paths * path_tiles);
@@ -63,8 +66,8 @@ Shape shape_of(int64_t problems, int64_t N, int64_t rows, int64_t head_dim, int6
     const double groups = (double)problems * prompt_tiles * s + (double)paths * path_tiles * t / (solo ? 4 : 1);
     const double values = (double)paths * rows * (s + t) * head_dim;
     const Cost cost = solo ? Cost{11400, 590, 640, 6700, 860} : Cost{11600, 410, 650, 7200, 420};
-    // (the longer items first, so that short ones are left for the end: 64 paths x 17 tokens of 4096 + 4096, which go through 43 and 64 blocks,
-    // 115 / 109 us; the others' prompts are first, 64 problems x 16 x 1 of 4096 + 512 240 / 254 us)
+    // (the longer items first, so that short ones are left for the end.  All of one kind before the other: 64 paths x 17 tokens of
+    // 4096 + 4096, 43 and 64 blocks, 115 us with the prompts first / 109; 64 problems x 16 x 1 of 4096 + 512, 64 and 16 blocks, 240 / 254)
     const bool paths_first = path_rounds > prompt_rounds;
     offer(Shape{kParts, solo, paths_first, prompt_tiles, path_tiles, s, t}, cost(prompt_rounds > path_rounds ? prompt_rounds : path_rounds, all, groups, values));
   }
@@ -73,7 +76,14 @@ Shape shape_of(int64_t problems, int64_t N, int64_t rows, int64_t head_dim, int6
 
 }  // namespace
 
-void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound, int32_t path_bound, int64_t parts, hipStream_t st) {
+// Either axis is split into no more than kItems / items + 1 parts, and items of up to 128 rows: kItems * 128 parts more than there are
+// rows.  (Short axes take fewer; never less than half of it is kept.)
+int64_t parts_of_rows(int64_t rows, int32_t prompt_cap, int32_t path_cap) {
+  const int64_t most = rows * (over(over(prompt_cap, kBlock), kLeastBlocks) + over(over(path_cap, kBlock), kLeastBlocks)), more = most - 2 * rows;
+  return 2 * rows + (more < kItems * 128 ? kItems * 128 : more < 2 * kItems * 128 ? more : 2 * kItems * 128);
+}
+
+void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound, int32_t path_bound, hipStream_t st) {
   const int64_t prompt_blocks = over(prompt_bound, kBlock), path_blocks = over(path_bound, kBlock);
   const int64_t paths = (int64_t)a.P * a.N * a.Hk, problems = (int64_t)a.P * a.Hk;
   const Shape shape = shape_of(problems, a.N, a.n * a.G, cfg.head_dim, prompt_blocks, path_blocks);
@@ -84,10 +94,6 @@ void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound,
   a.path_tiles = (int32_t)shape.path_tiles;
   a.prompt_splits = (int32_t)shape.prompt_splits;
   a.path_splits = (int32_t)shape.path_splits;
-  while ((int64_t)(a.prompt_splits + a.path_splits) * a.rows > parts) {
-    if (a.prompt_splits > a.path_splits) --a.prompt_splits;
-    else --a.path_splits;
-  }
   const int64_t chunks = problems * a.prompt_splits;
   a.prompt_turns = chunks % 8 == 0 || chunks >= 64;
   a.path_turns = a.how == kDirect && !a.solo && (problems % 8 == 0 || problems >= 64);
