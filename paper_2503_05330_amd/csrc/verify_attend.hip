@@ -94,9 +94,14 @@ void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound,
   a.path_tiles = (int32_t)shape.path_tiles;
   a.prompt_splits = (int32_t)shape.prompt_splits;
   a.path_splits = (int32_t)shape.path_splits;
+  // Items that have tokens in common go to one XCD, whose L2 then holds them once, unless that
+  // takes an eighth more turns of the eight's 64 workgroups.  (Paths with their whole prompt, 11 problems x 4 kv heads x 7 paths of 3000 + 700: 77 us dealt to
+  // all / 52 to one; 7 x 4 x 16 of 1024 + 1024 59 / 52; but 3 x 12 x 13 of 777 + 333, 65 items where 64 fit, 16.7 / 19.2.  Tiles of a
+  // prompt alone: the same from ten to sixty of them.)
   const int64_t chunks = problems * a.prompt_splits;
   a.prompt_turns = chunks % 8 == 0 || chunks >= 64;
-  a.path_turns = a.how == kDirect && !a.solo && (problems % 8 == 0 || problems >= 64);
+  const int64_t items = (int64_t)a.N * a.path_tiles;
+  a.path_turns = a.how == kDirect && !a.solo && 8 * over(over(problems, 8) * items, 64) <= 9 * over(problems * items, 512);
   const int64_t prompt_groups = a.prompt_turns ? over(chunks, 8) * 8 * a.prompt_tiles : chunks * a.prompt_tiles;
   const int64_t path_items = a.path_turns ? over(problems, 8) * 8 * a.N * a.path_tiles : paths * a.path_tiles * a.path_splits;
   AttendLaunch how{0, a.how == kParts, cfg.type == CSD_F16, cfg.fp8 != 0};
