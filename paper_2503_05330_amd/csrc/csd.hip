@@ -6,7 +6,7 @@
 // aggregated edge weights (Eq. 5), greedy layer-wise extraction (rule after
 // Eq. 5, Algorithm 1), and the greedy acceptance check ("Draft acceptance").
 //
-// Nothing here is a dense contraction, so there is no MFMA: the work is
+// Nothing of drafting is a dense contraction, so there is no MFMA: the work is
 // integer compares, hash lookups, LDS hash-histogram atomics and wavefront
 // reductions.  The step is latency-bound (a chain of a few dependent memory
 // round trips per path, then the serial work of one wave), so the design

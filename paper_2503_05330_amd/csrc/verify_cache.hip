@@ -3,7 +3,7 @@
 // A workgroup takes eight tokens of one row, its waves the kv heads, which lie side by side in a projection's output.  Eight
 // lanes hold a token, so that its largest value is found in three exchanges; a lane has 16 values of each 128 of a token,
 // 16 bytes of codes.  Long calls are bound by the copy: 8 prompts of up to 4096 tokens (half of them there), 8 heads of 128, are written
-// to 8 bits in 22.4 us and read back, with zeros for the missing, in 36.1: 4.5 and 4.7 TB/s.  Short ones are bound by the launch
+// to 8 bits in 25.5 us and read back, with zeros for the missing, in 28.1: 4.9 and 6.4 TB/s.  Short ones are bound by the launch
 // and the loads before a row's place is known: 64 x 16 paths of up to 9 tokens, 8 heads of 128, take 10.1 us to 8 bits (15.5 where
 // maxima and codes are taken in 32 bits; the type's own comparisons and conversion do two values an instruction, and exactly
 // that while all are finite).

