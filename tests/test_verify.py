@@ -295,6 +295,12 @@ def test_scores_far_below_and_above_zero(gen):
         check_attend(gen, 1, 2, 3, 4, 2, 64, [100], [[64, 61]], None, poison=poison, scale=scale)
 
 
+@pytest.mark.parametrize("dtype", [BF, F16])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_scale_of_zero_weighs_all_that_is_seen_alike(gen, dtype, fp8):
+    check_attend(gen, 1, 2, 3, 4, 2, 128, [100], [[64, 61]], None, dtype=dtype, fp8=fp8, scale=0.0)
+
+
 def test_a_cache_beyond_32_bit_offsets(gen):
     """A path whose keys and values start behind 4 GB, and one of a million tokens that all weigh the same."""
     U, D, Hk = 1 << 20, 128, 4
