@@ -256,6 +256,22 @@ def test_attention(gen, shape, dtype, fp8):
 
 
 @pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("P,N,H,Hk,prompt,path", [(33, 8, 4, 4, 573, 16), (33, 31, 8, 8, 36, 31), (13, 4, 8, 8, 1143, 251), (13, 6, 8, 8, 1104, 553)])
+def test_more_items_of_prompts_and_of_paths_than_are_dealt_at_once(gen, P, N, H, Hk, prompt, path, fp8):
+    """Some hundred workgroups each of prompts' and of paths' items, the longer ones the prompts' or the paths'."""
+    lengths = [prompt - 31 * p % prompt for p in range(P)]
+    paths = [[1 + (p * N + i) * 53 % path for i in range(N)] for p in range(P)]
+    counts = [[int((p + i) % 5 > 0) for i in range(N)] for p in range(P)]
+    check_attend(gen, P, N, 1, H, Hk, 64, lengths, paths, counts, fp8=fp8, caps=(prompt, path))
+
+
+@pytest.mark.parametrize("P,N,n,H,Hk,D", [(7, 5, 2, 8, 2, 64), (15, 3, 3, 4, 1, 128), (23, 2, 4, 8, 1, 64)])
+def test_problems_and_heads_that_are_no_multiple_of_eight(gen, P, N, n, H, Hk, D):
+    paths = [[n + (p * N + i) * 7 % 30 for i in range(N)] for p in range(P)]
+    check_attend(gen, P, N, n, H, Hk, D, [9 * p % 66 for p in range(P)], paths, None, caps=(65, 40))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("caps", [(64, 64), (2048, 64), (640, 1024)])
 def test_lengths_anywhere_below_the_capacities(gen, caps, fp8):
     """A launch is shaped by the capacities, or by the bounds; lengths are what they are."""
