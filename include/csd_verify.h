@@ -58,7 +58,8 @@ typedef struct {
                           bits, 3 of mantissa, largest 448) and a scale for each token and kv
                           head, keys and values apart: with a the largest finite |x| of the
                           head_dim values, s = the least power of two with a <= 448 s, but at
-                          least 2^-126 (1 where a = 0); code = x / s rounded to nearest even.
+                          least 2^-126 (1 where a = 0; half precision: 2^-32 where all values are
+                          zero); code = x / s rounded to nearest even.
                           Infinities become +-448 s, NaN stays NaN.  A power of two loses
                           nothing in a floating format, and x / s and code * s are exact.   */
 } csd_cache_config;

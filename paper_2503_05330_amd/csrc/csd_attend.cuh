@@ -14,7 +14,8 @@
 //
 // 8-bit values are multiplied without their scales 2^e, which go into P: P 2^e is as exact in bfloat16 as P.  Half precision
 // has not the range: there the exponent is added to the score, x = s + e, so that P = 2^(x - m) with m the maximum of x
-// is at most 2^8 whatever the scales are, and l sums P 2^-e.  Keys' scales go into the conversion to 16 bits, which takes a
+// is at most 2^8 whatever the scales are, and l sums P 2^-e; tokens whose values are all zero have the least of all e, so
+// that m is of tokens that add something.  Keys' scales go into the conversion to 16 bits, which takes a
 // power of two a lane.
 //
 // Sums, maxima and O are in 32 bits.  P is rounded to the 16-bit type, to nearest, for the second product (the matrix

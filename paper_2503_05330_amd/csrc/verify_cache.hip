@@ -47,6 +47,15 @@ __device__ inline uint32_t scale_exponent(float a) {
   return e < 1 ? 1 : (uint32_t)e;
 }
 
+// That of a token all of whose values are zero.  Any would do for them, but attention in half precision adds values' exponents to
+// scores and rounds weights beside the largest sum: so that a token which adds nothing does not make the others' weights small,
+// it gets the least exponent of any half, 2^-24.
+template <class T>
+__device__ inline uint32_t scale_exponent_of(uint32_t most_bits, float most) {
+  constexpr uint32_t kLeast = 127 - 24 - 8;
+  return T::kExponent == F16::kExponent && most_bits == 0 ? kLeast : scale_exponent(most);
+}
+
 // Eight values quantised by a power of two, each rounded once, to nearest; SOME_ODD: there may be infinities, which become the
 // largest code.
 template <class T, bool SOME_ODD>
@@ -141,7 +150,7 @@ __global__ __launch_bounds__(64 * kMoveWaves) void cache_write_kernel(MoveArgs a
         k_most = over_token(largest_finite<T>(k));
         v_most = over_token(largest_finite<T>(v));
       }
-      const uint32_t k_exp = scale_exponent(k_most), v_exp = scale_exponent(v_most);
+      const uint32_t k_exp = scale_exponent_of<T>(k_bits, k_most), v_exp = scale_exponent_of<T>(v_bits, v_most);
       const float k_scale = __uint_as_float(k_exp << 23), v_scale = __uint_as_float(v_exp << 23);
       if (!at.live) continue;
       if ((threadIdx.x & 7) == 0) {
