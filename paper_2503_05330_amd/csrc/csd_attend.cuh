@@ -13,10 +13,13 @@
 // O by 2^(m_old - m_new) needs no exchange; two lanes exchange one value per block for the maximum.
 //
 // 8-bit values are multiplied without their scales 2^e, which go into P: P 2^e is as exact in bfloat16 as P.  Half precision
-// has not the range: there the exponent is added to the score, x = s + e, so that P = 2^(x - m) with m the maximum of x
-// is at most 2^8 whatever the scales are, and l sums P 2^-e; tokens whose values are all zero have the least of all e, so
+// has not the range: there the exponent is added to the score, x = s + e, and P = 2^(x - m) with m of the maximum of x,
+// whatever the scales are, and l sums P 2^-e; tokens whose values are all zero have the least of all e, so
 // that m is of tokens that add something.  Keys' scales go into the conversion to 16 bits, which takes a
 // power of two a lane.
+//
+// Weights of half precision lose bits below 2^-14 and end at 2^-24, while l, in 32 bits, counts them all; so m is 7 less than the
+// maximum, weights go up to 2^15, and what is lost is below 2^-32 of the largest.
 //
 // Sums, maxima and O are in 32 bits.  P is rounded to the 16-bit type, to nearest, for the second product (the matrix
 // cores take no other): the weights of a row have errors of either sign that are as small as the output's own rounding.
@@ -75,7 +78,7 @@ struct Wave {
   typedef typename T::Eight Eight;
   typedef Rows<D, FP8> R;
   static constexpr int kTiles = D / 32;                  // of O's rows
-  static constexpr float kSlack = 8;
+  static constexpr float kSlack = 8, kLift = T::kExponent == F16::kExponent ? 7 : 0;
 
   Acc o[kTiles];
   Eight q[D / 16];
@@ -149,9 +152,10 @@ struct Wave {
         most = fmaxf(most, s[e][r]);
       }
     most = kAdded ? both_max(most) : both_max(most) * scale;
-    // m is the maximum when it was last set: weights may grow to 2^kSlack before O is rescaled, which few blocks behind the first do
-    if (__ballot(most > m + kSlack)) {                   // (m -inf: nothing has been summed)
-      const float high = fmaxf(m, most), down = m == kNone ? 0.0f : exp2_fast(m - high);
+    // m is the maximum when it was last set, less kLift: weights may grow to 2^(kSlack + kLift) before O is rescaled, which few blocks
+    // behind the first do
+    if (__ballot(most > m + (kSlack + kLift))) {         // (m -inf: nothing has been summed)
+      const float high = fmaxf(m, most - kLift), down = m == kNone ? 0.0f : exp2_fast(m - high);
       l *= down;
 #pragma unroll
       for (int x = 0; x < kTiles; ++x) o[x] *= down;

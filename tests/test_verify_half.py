@@ -56,3 +56,10 @@ def check(gen, fp8, size, gap, T, U, at, n=2, H=4, spread=0.3, one=False):
 @pytest.mark.parametrize("of_path", [False, True])
 def test_a_token_without_values_in_an_8_bit_cache(gen, size, gap, T, U, of_path):
     check(gen, True, size, gap, T, U, T + 11 if of_path else 5)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,U,at,n,H", [(40, 30, 3, 2, 4), (40, 30, 60, 2, 4), (300, 100, 130, 17, 8), (0, 64, 40, 2, 8)])
+def test_weights_below_the_range_of_half(gen, fp8, T, U, at, n, H):
+    """All weights but one are 2^-26 of that one."""
+    check(gen, fp8, 1000.0, 18, T, U, at, n, H, spread=0.1, one=True)
