@@ -17,6 +17,7 @@
 #include <ATen/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 
 #include "csd.h"
@@ -66,11 +67,12 @@ struct Call {
     usual = false;
     return 0;
   }
+  // (nor one that a gradient is wanted of: verify.py raises)
   const at::Tensor* any_tensor(bool maybe = false) {
     PyObject* o = next();
     if (THPVariable_CheckExact(o)) {
       const at::Tensor& t = THPVariable_Unpack(o);
-      if (t.is_cuda()) return &t;
+      if (t.is_cuda() && !(t.requires_grad() && c10::GradMode::is_enabled())) return &t;
     }
     usual = usual && maybe && o == Py_None;
     return nullptr;

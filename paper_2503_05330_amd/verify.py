@@ -5,7 +5,7 @@ behind it.  PathCache holds the keys and values of the prompts, which the paths 
 bits or quantised to 8 as they are written, and attends to them; targets() turns the logits into the tokens that
 Index.accept compares with, and the probabilities that Index.append and Index.step take.  Argument marshalling only, in
 native code (_csd_torch.so) where the arguments are the usual ones: all of it runs in the HIP kernels of libcsd.so, on the
-current stream.
+current stream.  Serving only: there are no gradients, and a tensor that requires one is refused unless gradients are off.
 """
 from __future__ import annotations
 
@@ -67,6 +67,11 @@ def _check(rc: int, what: str) -> None:
         raise CsdError(rc, what)
 
 
+def _no_gradients(*tensors) -> None:
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise TypeError("no gradients here: call under torch.no_grad(), or with detached tensors")
+
+
 def _spacing(shape, stride) -> int:
     """The distance of the rows of leading axes that are evenly spaced (0: there is one row)."""
     rows, spacing = 1, 0
@@ -83,6 +88,7 @@ def _heads(t: torch.Tensor, dtype, lead, n_heads: int, dim: int) -> Heads:
     """A tensor [*lead][n][heads][dim]: dense, or a slice of tokens or heads of a larger one."""
     if not t.is_cuda or t.dtype != dtype:
         raise TypeError("expected a device tensor of dtype %s" % dtype)
+    _no_gradients(t)
     shape, stride, at = tuple(t.shape), t.stride(), len(lead)
     if shape[:at] != tuple(lead) or len(shape) != at + 3 or shape[-2:] != (n_heads, dim):
         raise ValueError("tensor of shape %s, needs %s" % (shape, (*lead, "n", n_heads, dim)))
@@ -191,6 +197,7 @@ class PathCache:
             if got is not None:
                 _check(got[0], "csd_attend")
                 return got[1]
+        _no_gradients(out, lse)
         c, rows = self.cfg, self.P * self.N
         heads = _heads(q, self.dtype, (self.P, self.N), c.n_heads, c.head_dim)
         n = q.shape[2]
@@ -226,6 +233,7 @@ def targets(logits: torch.Tensor, noise: Optional[torch.Tensor] = None, inv_temp
     for t in (logits,) if noise is None else (logits, noise):
         if not t.is_cuda or t.dim() == 0 or (t.stride(-1) != 1 and t.shape[-1] > 1):
             raise TypeError("expected a device tensor with contiguous rows")
+    _no_gradients(logits, noise)
     lead, vocab = logits.shape[:-1], logits.shape[-1]
     rows, stride = lead.numel(), _spacing(lead, logits.stride())
     noise_stride = _spacing(lead, noise.stride()) if noise is not None else 0
