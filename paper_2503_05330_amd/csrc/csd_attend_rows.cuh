@@ -77,6 +77,10 @@ __device__ inline const uint8_t* uniform(const uint8_t* p) {
   return reinterpret_cast<const uint8_t*>((uint64_t)high << 32 | (uint64_t)low);
 }
 
+// (m0 is named as written, so that the compiler sets it again where it wants a value there.  It warns of that: m0 is reserved, it
+// never keeps it for a program.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 // N pieces of 1 KB from piece p on
 template <class R, int N>
 __device__ inline void fetch(uint32_t lds, const uint8_t* from, int p, uint32_t source) {
@@ -85,22 +89,23 @@ __device__ inline void fetch(uint32_t lds, const uint8_t* from, int p, uint32_t 
         "s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
         "global_load_lds_dwordx4 %2, %5 offset:1024\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048\n\t"
         "global_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds), "v"(source ^ R::turn(p)), "v"(source ^ R::turn(p + 1)),
-        "v"(source ^ R::turn(p + 2)), "v"(source ^ R::turn(p + 3)), "s"(from) : "memory");
+        "v"(source ^ R::turn(p + 2)), "v"(source ^ R::turn(p + 3)), "s"(from) : "m0", "memory");
     if constexpr (N > 4) fetch<R, N - 4>(lds + 4096, from + 4096, p + 4, source);
   } else if constexpr (N >= 2) {
     asm volatile(
         "s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
-        "global_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds), "v"(source ^ R::turn(p)), "v"(source ^ R::turn(p + 1)), "s"(from) : "memory");
+        "global_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds), "v"(source ^ R::turn(p)), "v"(source ^ R::turn(p + 1)), "s"(from) : "m0", "memory");
     if constexpr (N > 2) fetch<R, N - 2>(lds + 2048, from + 2048, p + 2, source);
   } else {
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(source ^ R::turn(p)), "s"(from) : "memory");
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(source ^ R::turn(p)), "s"(from) : "m0", "memory");
   }
 }
 // 64 bytes, 4 from each of the first sixteen lanes
 __device__ inline void fetch_scales(uint32_t lds, const uint8_t* from, int lane) {
   if (lane < 16)
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(lane * 4), "s"(from) : "memory");
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(lane * 4), "s"(from) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 // until no more than N of the wave's loads are under way
 template <int N>
 __device__ inline void wait_loads() {
