@@ -61,7 +61,10 @@ typedef struct {
                           least 2^-126 (1 where a = 0; half precision: 2^-32 where all values are
                           zero); code = x / s rounded to nearest even.
                           Infinities become +-448 s, NaN stays NaN.  A power of two loses
-                          nothing in a floating format, and x / s and code * s are exact.   */
+                          nothing in a floating format, and x / s and code * s are exact.
+                          (Half precision: |x| of 63488 and more are held as 65536, an infinity
+                          beside a > 57344 as 114688.  csd_attend works with these numbers;
+                          csd_cache_read rounds them to half, to infinity.)                 */
 } csd_cache_config;
 
 /* Rows of tokens of heads: element d of head h of token t of row r is data[r * row_stride + t * token_stride + h * head_stride + d],

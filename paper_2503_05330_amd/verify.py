@@ -178,7 +178,8 @@ class PathCache:
         return k, v
 
     def read(self, layer, n, start=None, counts=None):
-        """Keys and values [P][N][n][kv heads][head_dim] of the paths, rows as in write(); zero beyond a row's count."""
+        """Keys and values [P][N][n][kv heads][head_dim] of the paths, rows as in write(); zero beyond a row's count.  (8 bits of
+        float16: 63488 and more are held as 65536, which attend() works with and read() gives as infinity.)"""
         return self._read(_lib.csd_cache_read, "csd_cache_read", (self.P, self.N), layer, n, start, counts)
 
     def read_prompt(self, layer, n, start=None, counts=None):

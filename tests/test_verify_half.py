@@ -63,3 +63,19 @@ def test_a_token_without_values_in_an_8_bit_cache(gen, size, gap, T, U, of_path)
 def test_weights_below_the_range_of_half(gen, fp8, T, U, at, n, H):
     """All weights but one are 2^-26 of that one."""
     check(gen, fp8, 1000.0, 18, T, U, at, n, H, spread=0.1, one=True)
+
+
+@pytest.mark.parametrize("value", [63456.0, 63488.0, 65504.0, -65504.0, float("inf")])
+def test_the_largest_numbers_of_half_in_an_8_bit_cache(gen, value):
+    """63488 and more are held as 65536, an infinity as 448 times the scale of 256: attention works with what is held, reading
+    back rounds it to half."""
+    c = verify.PathCache(1, 1, 0, 4, 2, 1, 64, 1, dtype=F16, fp8=True)
+    k, v = torch.zeros((1, 1, 4, 1, 64), dtype=F16, device="cuda"), torch.zeros((1, 1, 4, 1, 64), dtype=F16, device="cuda")
+    v[0, 0, 1, 0, :2] = torch.tensor([value, 60000.0])
+    c.write(0, k, v)
+    stands_for = held(v, True)
+    assert stands_for[0, 0, 1, 0, 0].abs() == {63456.0: 61440, float("inf"): 448 * 256}.get(value, 65536)
+    assert torch.equal(c.read(0, 4)[1].cpu(), stands_for.to(F16))
+    out = c.attend(0, normal(gen, (1, 1, 1, 2, 64), F16), None, ints([[4]])).double().cpu()
+    want = stands_for[0, 0].sum(0) / 4                   # four equal weights
+    assert ((out[0, 0, 0] - want).abs() <= ROUND[F16] * want.abs()).all()
