@@ -122,6 +122,17 @@ int csd_attend(csd_cache* cache, int32_t layer, const csd_heads* q, const int32_
                const int32_t* d_counts, int32_t n, float scale, int32_t prompt_bound, int32_t path_bound, void* d_out, float* d_lse,
                void* stream);
 
+/* The form of the launch that csd_attend makes of a call with these sizes (nothing is enqueued; prompt_bound, path_bound as there). */
+typedef struct {
+  int32_t joined;        /* 0: each path with its whole prompt.  1: parts of the prompts, of a problem's paths together, and of the
+                            paths, which a second launch joins */
+  int32_t solo;          /* a path's rows are a wave's, up to 32 of them, instead of a workgroup's, up to 128 */
+  int32_t prompt_splits; /* parts of a prompt's tokens (0: not joined, or no prompt) */
+  int32_t path_splits;   /* parts of a path's tokens */
+  int32_t groups;        /* workgroups */
+} csd_attend_form;
+int csd_attend_form_of(const csd_cache_config* cfg, int32_t n, int32_t prompt_bound, int32_t path_bound, csd_attend_form* out_form);
+
 /* The token that the model picks in each row of logits, and the probability that it gives it.
  *   d_logits [rows][vocab] of `type` (CSD_BF16, CSD_F16, CSD_F32), rows logit_stride elements apart
  *   d_noise  [rows][vocab] float, rows noise_stride elements apart; NULL = greedy

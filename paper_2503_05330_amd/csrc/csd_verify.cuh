@@ -131,8 +131,9 @@ void attend_96(const AttendArgs& a, const AttendLaunch& how, hipStream_t st);
 void attend_128(const AttendArgs& a, const AttendLaunch& how, hipStream_t st);
 void attend_256(const AttendArgs& a, const AttendLaunch& how, hipStream_t st);
 
-// The bounds are of the lengths.
-void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound, int32_t path_bound, hipStream_t st);
+// The bounds are of the lengths, 0 the capacities.  attend_form() sets a's sizes and form of launch for n tokens a path.
+AttendLaunch attend_form(AttendArgs* a, const csd_cache_config& cfg, int32_t n, int32_t prompt_bound, int32_t path_bound);
+void attend_any(const AttendArgs& a, const AttendLaunch& how, int32_t head_dim, hipStream_t st);
 // How many parts calls of so many rows write at most.
 int64_t parts_of_rows(int64_t rows, int32_t prompt_cap, int32_t path_cap);
 void cache_write(const MoveArgs& a, int32_t head_dim, bool f16, bool fp8, hipStream_t st);

@@ -201,28 +201,31 @@ int csd_attend(csd_cache* cache, int32_t layer, const csd_heads* q, const int32_
   if (!d_path_len || !d_out || misaligned(d_out) || !std::isfinite(scale) || prompt_bound < 0 || path_bound < 0) return CSD_ERR_INVALID_ARG;
   const csd_cache_config& cfg = cache->cfg;
   AttendArgs a;
+  const AttendLaunch how = attend_form(&a, cfg, n, prompt_bound, path_bound);
   a.prompt = cache->held(true, layer);
   a.path = cache->held(false, layer);
   a.q = *q;
   a.prompt_len = d_prompt_len;
   a.path_len = d_path_len;
   a.counts = d_counts;
-  a.P = cfg.n_problems;
-  a.N = cfg.n_paths;
-  a.n = n;
-  a.H = cfg.n_heads;
-  a.Hk = cfg.n_kv_heads;
-  a.G = cfg.n_heads / cfg.n_kv_heads;
   a.scale = scale * 1.44269504088896340736f;
   a.out = d_out;
   a.lse = d_lse;
   a.part_o = reinterpret_cast<float*>(cache->base + cache->layout.part_o);
   a.part_lse = reinterpret_cast<float*>(cache->base + cache->layout.part_lse);
-  a.rows = (int64_t)a.P * a.N * n * a.H;
-  if (prompt_bound == 0 || prompt_bound > cfg.prompt_cap) prompt_bound = cfg.prompt_cap;
-  if (path_bound == 0 || path_bound > cfg.path_cap) path_bound = cfg.path_cap;
-  attend_any(a, cfg, prompt_bound, path_bound, static_cast<hipStream_t>(stream));
+  attend_any(a, how, cfg.head_dim, static_cast<hipStream_t>(stream));
   return finish("csd_attend");
+}
+
+int csd_attend_form_of(const csd_cache_config* cfg, int32_t n, int32_t prompt_bound, int32_t path_bound, csd_attend_form* out_form) {
+  using namespace csd::verify;
+  const int rc = check(cfg);
+  if (rc != CSD_OK) return rc;
+  if (n <= 0 || n > cfg->max_step || prompt_bound < 0 || path_bound < 0 || !out_form) return CSD_ERR_INVALID_ARG;
+  AttendArgs a;
+  const AttendLaunch how = attend_form(&a, *cfg, n, prompt_bound, path_bound);
+  *out_form = csd_attend_form{how.join, a.solo, a.prompt_splits, a.path_splits, (int32_t)how.groups};
+  return CSD_OK;
 }
 
 int csd_cache_status(csd_cache* cache, uint32_t* host_flags, void* stream) {

@@ -9,15 +9,6 @@ namespace {
 
 int64_t over(int64_t x, int64_t y) { return (x + y - 1) / y; }
 
-void attend_dim(const AttendArgs& a, const AttendLaunch& how, int32_t head_dim, hipStream_t st) {
-  switch (head_dim) {
-    case 64: return attend_64(a, how, st);
-    case 96: return attend_96(a, how, st);
-    case 128: return attend_128(a, how, st);
-    default: return attend_256(a, how, st);
-  }
-}
-
 struct Shape {
   int32_t how;
   bool solo, paths_first;
@@ -96,7 +87,17 @@ int64_t parts_of_rows(int64_t rows, int32_t prompt_cap, int32_t path_cap) {
   return 2 * rows + (more < kLeast ? kLeast : more < kMost ? more : kMost);
 }
 
-void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound, int32_t path_bound, hipStream_t st) {
+AttendLaunch attend_form(AttendArgs* args, const csd_cache_config& cfg, int32_t n, int32_t prompt_bound, int32_t path_bound) {
+  AttendArgs& a = *args;
+  a.P = cfg.n_problems;
+  a.N = cfg.n_paths;
+  a.n = n;
+  a.H = cfg.n_heads;
+  a.Hk = cfg.n_kv_heads;
+  a.G = cfg.n_heads / cfg.n_kv_heads;
+  a.rows = (int64_t)a.P * a.N * n * a.H;
+  if (prompt_bound == 0 || prompt_bound > cfg.prompt_cap) prompt_bound = cfg.prompt_cap;
+  if (path_bound == 0 || path_bound > cfg.path_cap) path_bound = cfg.path_cap;
   const int64_t prompt_blocks = over(prompt_bound, kBlock), path_blocks = over(path_bound, kBlock);
   const int64_t paths = (int64_t)a.P * a.N * a.Hk, problems = (int64_t)a.P * a.Hk;
   const Shape shape = shape_of(problems, a.N, a.n * a.G, prompt_blocks, path_blocks, cfg.head_dim, cfg.fp8);
@@ -120,7 +121,16 @@ void attend_any(AttendArgs a, const csd_cache_config& cfg, int32_t prompt_bound,
   AttendLaunch how{0, a.how == kParts, cfg.type == CSD_F16, cfg.fp8 != 0};
   a.prompt_groups = a.how == kParts ? (int32_t)prompt_groups : 0;
   how.groups = (uint32_t)(a.prompt_groups + (a.solo ? over(path_items, 4) : path_items));
-  attend_dim(a, how, cfg.head_dim, st);
+  return how;
+}
+
+void attend_any(const AttendArgs& a, const AttendLaunch& how, int32_t head_dim, hipStream_t st) {
+  switch (head_dim) {
+    case 64: return attend_64(a, how, st);
+    case 96: return attend_96(a, how, st);
+    case 128: return attend_128(a, how, st);
+    default: return attend_256(a, how, st);
+  }
 }
 
 }  // namespace verify

@@ -21,7 +21,7 @@ BF16, F16, F32 = 0, 1, 2
 TYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 
 EXPORTS = ["csd_cache_bytes", "csd_cache_create", "csd_cache_destroy", "csd_cache_write", "csd_cache_write_prompt",
-           "csd_cache_read", "csd_cache_read_prompt", "csd_attend", "csd_targets_bytes", "csd_targets", "csd_cache_status"]
+           "csd_cache_read", "csd_cache_read_prompt", "csd_attend", "csd_attend_form_of", "csd_targets_bytes", "csd_targets", "csd_cache_status"]
 
 
 class CacheConfig(ctypes.Structure):
@@ -32,6 +32,10 @@ class CacheConfig(ctypes.Structure):
 
 class Heads(ctypes.Structure):
     _fields_ = [("data", _vp)] + [(name, ctypes.c_int64) for name in ("row_stride", "token_stride", "head_stride")]
+
+
+class AttendForm(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("joined", "solo", "prompt_splits", "path_splits", "groups")]
 
 
 _lib = None
@@ -53,6 +57,7 @@ def load() -> ctypes.CDLL:
         for name in ("csd_cache_read", "csd_cache_read_prompt"):
             getattr(lib, name).argtypes = [_vp, i32, _vp, _vp, i32, _vp, _vp, _vp]
         lib.csd_attend.argtypes = [_vp, i32, heads, _vp, _vp, _vp, i32, f32, i32, i32, _vp, _vp, _vp]
+        lib.csd_attend_form_of.argtypes = [cfgp, i32, i32, i32, ctypes.POINTER(AttendForm)]
         lib.csd_targets_bytes.argtypes = [i64, i32, ctypes.POINTER(size)]
         lib.csd_targets.argtypes = [_vp, i32, i64, i32, i64, _vp, i64, f32, _vp, _vp, _vp, size, _vp]
         lib.csd_cache_status.argtypes = [_vp, ctypes.POINTER(ctypes.c_uint32), _vp]
@@ -98,6 +103,13 @@ def _heads(t: torch.Tensor, dtype, lead, n_heads: int, dim: int) -> Heads:
     if (h.data or 0) % 16 or h.row_stride % 8 or h.token_stride % 8 or h.head_stride % 8:
         raise ValueError("heads must start at multiples of 16 bytes")
     return h
+
+
+def attend_form(cfg: CacheConfig, n: int, prompt_bound: int = 0, path_bound: int = 0) -> AttendForm:
+    """The form of the launch of PathCache.attend() for n tokens a path (host only: no GPU is needed)."""
+    form = AttendForm()
+    _check(load().csd_attend_form_of(ctypes.byref(cfg), n, prompt_bound, path_bound, ctypes.byref(form)), "csd_attend_form_of")
+    return form
 
 
 class PathCache:
