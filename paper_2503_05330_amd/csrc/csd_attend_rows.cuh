@@ -14,7 +14,9 @@
 // part.  64 problems x 16 paths x 1 token over 4096 + 512 (8-bit, 32 heads of 128 on 8) 229 us, 4.9 TB/s; x 9 over 1024 + 1024
 // 432 us, 3.9 TB/s, 400 without any arithmetic; 64 paths x 17 over 4096 + 4096 (16-bit, 28 heads on 4) 102 us, 4.0 TB/s and
 // 430 TFLOP/s, 92 without arithmetic.  Small ones: the launch and round trips that depend on each other, lengths, queries and
-// first blocks, results: 4 paths x 1 over 256 + 64 takes 9 us, 16 x 1 over 1024 + 1024 19 us (2.5 TB/s).
+// first blocks, results: 4 paths x 1 over 256 + 64 takes 9 us, 16 x 1 over 1024 + 1024 19 us (2.5 TB/s).  Heads of 256 have one
+// workgroup a CU, and 50 .. 126 of their registers lie in scratch memory, which the loops reload: 16 x 9 over 1024 + 1024 (16-bit, 16
+// heads on 8) 45 us, 2.0 TB/s, 64 problems x 16 x 9 (8-bit) 757 us, 4.0 TB/s; of 96, 32 heads on 8, 23 and 381 us, 1.5 and 3.1 TB/s.
 #pragma once
 
 #include "csd_attend.cuh"

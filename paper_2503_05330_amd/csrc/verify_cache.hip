@@ -3,7 +3,8 @@
 // A workgroup takes eight tokens of one row, its waves the kv heads, which lie side by side in a projection's output.  Eight
 // lanes hold a token, so that its largest value is found in three exchanges; a lane has 16 values of each 128 of a token,
 // 16 bytes of codes.  Long calls are bound by the copy: 8 prompts of up to 4096 tokens (half of them there), 8 heads of 128, are written
-// to 8 bits in 25.5 us and read back, with zeros for the missing, in 28.1: 4.9 and 6.4 TB/s.  Short ones are bound by the launch
+// to 8 bits in 25.5 us and read back, with zeros for the missing, in 28.1: 4.9 and 6.4 TB/s; with all tokens there, the same input each
+// time, 30.4 and 33.4, in 16 bits 44.2 and 42.9: 6.1 .. 6.6 TB/s.  Short ones are bound by the launch
 // and the loads before a row's place is known: 64 x 16 paths of up to 9 tokens, 8 heads of 128, take 10.1 us to 8 bits (15.5 where
 // maxima and codes are taken in 32 bits; the type's own comparisons and conversion do two values an instruction, and exactly
 // that while all are finite).

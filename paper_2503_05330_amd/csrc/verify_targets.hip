@@ -2,10 +2,10 @@
 //
 // One pass: every thread keeps the largest y = x / T of the softmax and the sum of exp(y - largest), and the largest z (y + noise, or
 // the logit itself) with its place, over vectors of 16 bytes; the two maxima are compared a vector at a time and change
-// rarely, so what an element costs is its conversion, a product, a sum and an exponential.  exp is taken of differences
-// that are rounded once, so that a token's probability has an error of a few 2^-24.  Where there are fewer rows than it takes
+// rarely, so what an element costs is its conversion, a product, a sum and an exponential.  y and its difference to the
+// largest are rounded once each before exp, so that a token's probability has a relative error of a few (|y| + |y - largest| + 1) 2^-24.  Where there are fewer rows than it takes
 // to fill the chip a row is shared by several workgroups (`parts`) and a second launch joins them.  Bound by memory: 1088 rows of 152064
-// 16-bit logits with noise 166 us, 6.0 TB/s; 4 rows of 32000, 7.3 us, by the launch and the latency of 16 vectors a thread.
+// 16-bit logits with noise 166 us, 6.0 TB/s; 4 rows of 32000, 7.3 us, by the launch and the latency of 8 vectors a thread, four at a time.
 #include "csd_launch.h"
 #include "csd_verify.cuh"
 
@@ -169,7 +169,9 @@ __global__ __launch_bounds__(64) void targets_join_kernel(TargetArgs a) {
 
 // Workgroups of a row.  Few rows of large vocabularies are shared by as many as make some 250 of 100000 logits, each of 2048 at
 // least (us in one launch / in two: 8 rows of 152064 20.9 / 7.9, 64 22.5 / 12.9, 128 22.8 / 17.3, 8 of 50257 9.8 / 7.7; but 4
-// rows of 32000 7.8 / 7.4, which the second launch costs a caller, and 2 of 16000 5.9 / 6.9).  Many rows of more than half a megabyte, logits and noise, are cut in
+// rows of 32000 7.8 / 7.4, which the second launch costs a caller, and 2 of 16000 5.9 / 6.9).  From 195 to 511 rows, where the rule gives
+// one each, two to four are slower or the same (256 of 152064 23.1 / 23.4, with noise 37 / 40; 256 of 50257 9.8 / 13) but around 320
+// (34 / 27, with noise 57 / 48), and 160 with noise get two where one is faster (25.5 / 33).  Many rows of more than half a megabyte, logits and noise, are cut in
 // eight, so that the last ones leave no CU idle (1088 rows of 152064 with noise 182 / 165, 768 126 / 119; 768 without
 // noise 52 / 63); so many that a launch would have more than 2^31 threads are not.
 constexpr int32_t kMostParts = 32, kLeastLogits = 2048, kLongParts = 8, kThreads = 512;
