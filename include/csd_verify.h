@@ -10,6 +10,11 @@
  *   csd_attend    attention of all paths' new tokens over that cache;
  *   csd_targets   the model's token at every position, with the probability that it gave it: what
  *                 csd_accept compares with and what csd_append / csd_step take as tokens and probabilities.
+ * and what stands around them in the model's own work:
+ *   csd_rotate    rotary positions on queries and keys; csd_cache_write_rotated: with the write to the cache, in one launch
+ *   csd_prompt_attend   attention of whole prompts to themselves, packed behind each other; csd_cache_write_packed
+ *                 puts their keys and values into the cache
+ *   csd_adjust    penalties for repeated tokens, biases and masks on the logits, before csd_targets.
  *
  * Conventions are those of csd.h: pointers named d_* (and csd_heads.data) are device memory of the caller, `stream` is a
  * hipStream_t as void*, calls only enqueue (except csd_cache_status), allocate nothing, can be captured in
@@ -31,7 +36,7 @@ extern "C" {
 /* Element types. */
 #define CSD_BF16 0
 #define CSD_F16 1
-#define CSD_F32 2 /* csd_targets only */
+#define CSD_F32 2 /* csd_targets and csd_adjust only */
 
 /* Limits of this build. */
 #define CSD_MAX_VERIFY_STEP (CSD_MAX_DRAFT_LEN + 1) /* tokens a path and csd_attend call */
@@ -39,7 +44,10 @@ extern "C" {
 #define CSD_MAX_HEADS 512
 #define CSD_MAX_LAYERS 1024
 #define CSD_MAX_ROW_TILES (1 << 21)   /* P * N * n_kv_heads * ceil(max_step * n_heads / n_kv_heads / 32) */
-#define CSD_MAX_TARGET_ROWS (1 << 22) /* rows of a csd_targets call */
+#define CSD_MAX_TARGET_ROWS (1 << 22) /* rows of a csd_targets or csd_adjust call */
+#define CSD_MAX_PACKED_TOKENS (1 << 24)             /* tokens of packed sequences, and of a csd_rotate call */
+#define CSD_MAX_SEQUENCES (1 << 20)
+#define CSD_MAX_ROTATED_DIM 512
 
 typedef struct csd_cache csd_cache; /* opaque, host-side, library-owned */
 
@@ -148,6 +156,92 @@ int csd_targets_bytes(int64_t rows, int32_t vocab, size_t* out_bytes);
 int csd_targets(const void* d_logits, int32_t type, int64_t rows, int32_t vocab, int64_t logit_stride, const float* d_noise,
                 int64_t noise_stride, float inv_temperature, int32_t* d_tokens, float* d_probs, void* d_scratch, size_t scratch_bytes,
                 void* stream);
+
+/* Rotary positions.  Pair i (of dim / 2) of a head at position t is turned by the angle 2 pi t turns[i]:
+ *   (a, b) -> amplitude * (a cos - b sin, a sin + b cos), in 32 bits, rounded once.
+ * Positions are whole numbers of any sign; turns and their product with a position are in 64 bits, so far positions lose nothing. */
+typedef struct {
+  const double* d_turns; /* [dim / 2], device memory, 8-byte aligned: turns per token (csd_rotary_turns makes the usual ones)  */
+  int32_t dim;           /* the first dim values of a head are rotated, the others copied: a multiple of 16, up to the head's   */
+  int32_t interleaved;   /* 0: pair i is (i, i + dim / 2), 1: (2 i, 2 i + 1)                                                   */
+  float amplitude;       /* finite; 1 as a rule                                                                               */
+} csd_rotary;
+
+/* The turns of a rotation, on the host: f_i = base^(-2i/dim) / (2 pi), and for contexts longer than those of the training f_i / factor;
+ * with original > 0, the training's length, r = original * f_i turns over it, keep = (r - low) / (high - low) within [0, 1]:
+ * f_i * (keep + (1 - keep) / factor), which leaves the fast pairs alone.  base > 1, factor > 0, original >= 0, high > low. */
+int csd_rotary_turns(int32_t dim, double base, double factor, double original, double low, double high, double* out_turns);
+
+/* Rotates `tokens` tokens of `heads` heads of `head_dim` values (a multiple of 8, up to CSD_MAX_ROTATED_DIM).
+ *   x, out       element d of head h of token t is data[t * token_stride + h * head_stride + d] (row_stride is not used); 16-byte aligned, strides
+ *                multiples of 8.  out may be x itself, with the same strides; else they must not overlap.
+ *   d_positions  [tokens] int32
+ *   type         CSD_BF16 or CSD_F16 */
+int csd_rotate(const csd_rotary* rotary, const csd_heads* x, const int32_t* d_positions, int64_t tokens, int32_t heads, int32_t head_dim,
+               int32_t type, const csd_heads* out, void* stream);
+
+/* csd_rotate of queries and keys and csd_cache_write of the rotated keys (rounded to the cache's type, as csd_rotate does) and the values, in one launch.
+ *   q, k, v      n tokens of each path, n_heads, n_kv_heads and n_kv_heads heads
+ *   d_positions  [P][N][n] int32
+ *   d_q_out      [P][N][n][n_heads][head_dim] dense, 16-byte aligned: all n tokens' rotated queries, whatever the counts; must not overlap q, k, v */
+int csd_cache_write_rotated(csd_cache* cache, int32_t layer, const csd_rotary* rotary, const csd_heads* q, const csd_heads* k, const csd_heads* v,
+                            const int32_t* d_positions, const int32_t* d_start, const int32_t* d_counts, int32_t n, void* d_q_out, void* stream);
+
+/* Sequences packed behind each other: sequence s has the tokens d_offsets[s] .. d_offsets[s + 1] - 1 of `tokens`; d_offsets ascends
+ * (an empty sequence is fine).  Offsets are clamped to [0, tokens]; where they descend, results are unspecified, but nothing outside
+ * of the tensors is touched.
+ *
+ * csd_cache_write_packed writes sequence p to the prompt of problem p, from position 0 on (P + 1 offsets): tokens beyond prompt_cap are dropped and
+ * raise CSD_STATUS_CAPACITY.  k, v: tokens of n_kv_heads heads (row_stride is not used). */
+int csd_cache_write_packed(csd_cache* cache, int32_t layer, const csd_heads* k, const csd_heads* v, const int32_t* d_offsets, int64_t tokens,
+                           void* stream);
+
+/* Attention of each sequence to itself: token t sees tokens 0 .. t of its sequence.
+ *   q, k, v  tokens of n_heads, n_kv_heads, n_kv_heads heads (row_stride is not used); n_heads is a multiple of n_kv_heads, up to CSD_MAX_HEADS
+ *   d_out    [tokens][n_heads][head_dim] dense, 16-byte aligned = sum_x softmax_x(scale * q.k_x) v_x, must not overlap q, k, v
+ *   d_lse    [tokens][n_heads] float = ln sum_x exp(scale * q.k_x), may be NULL
+ * Tokens of no sequence are not written.  Nothing that a token does not see, not even an infinity or a NaN, changes its result; where
+ * all that it sees weighs nothing (every score -inf), it gets zeros and -inf.
+ * head_dim 64, 96, 128 or 256 (else CSD_ERR_UNIMPLEMENTED), type CSD_BF16 or CSD_F16; token strides of k and v up to 2^24 elements;
+ * (tokens * n_heads / n_kv_heads / 128 + sequences) * n_kv_heads up to 2^23. */
+int csd_prompt_attend(const csd_heads* q, const csd_heads* k, const csd_heads* v, int32_t type, int32_t n_heads, int32_t n_kv_heads,
+                      int32_t head_dim, const int32_t* d_offsets, int32_t sequences, int64_t tokens, float scale, void* d_out, float* d_lse,
+                      void* stream);
+
+/* Logits of n positions of every path (n up to CSD_MAX_VERIFY_STEP) as they are sampled from.  Position t of path (p, i) has said the path's first
+ * path_len - count + t + 1 tokens (as in csd_attend: the n newest are the pass's own), and the prompt's.  For a token that was said c
+ * times by the path, in 32 bits, rounded once to the type:
+ *   x  = the logit
+ *   x  = x > 0 ? x / repetition : x * repetition   if c > 0 or the prompt has the token
+ *   x  = x - (frequency * c + presence)            if c > 0
+ *   x  = x + bias
+ *   x  = -inf                                      if the mask's bit is 0
+ * so a masked logit is -inf whatever it was.  A row of a position beyond its path's count becomes zeros. */
+typedef struct {
+  int32_t n_problems, n_paths, n, vocab; /* P, N, n, V                                                                          */
+  int32_t type;                          /* CSD_BF16, CSD_F16 or CSD_F32                                                       */
+  const void* d_logits;                  /* [P][N][n][V], rows logit_stride elements apart                                     */
+  int64_t logit_stride;
+  void* d_out;                           /* the same, rows out_stride apart; may be d_logits with the same stride              */
+  int64_t out_stride;
+  const int32_t* d_counts;               /* [P][N] how many of the n positions are a path's (clamped to [0, n]); NULL = n        */
+  const float* d_penalties;              /* [P][3] repetition (> 0), presence, frequency; NULL: none, and no tokens are read     */
+  const int32_t* d_tokens;               /* [P][N] rows of up to path_cap tokens, token_stride apart; NULL: none                */
+  int64_t token_stride;
+  int32_t path_cap;
+  const int32_t* d_path_len;             /* [P][N] the new ones among them (clamped to [0, path_cap]); NULL only without tokens  */
+  const int32_t* d_prompt;               /* [P] rows of up to prompt_cap tokens, prompt_stride apart; NULL: none               */
+  int64_t prompt_stride;
+  int32_t prompt_cap;
+  const int32_t* d_prompt_len;           /* [P] (clamped to [0, prompt_cap]); NULL = prompt_cap                                  */
+  const float* d_bias;                   /* [P][V], rows bias_stride apart (0: one for all); NULL: none                        */
+  int64_t bias_stride;
+  const uint32_t* d_mask;                /* [P][N][n] rows of (V + 31) / 32 words, mask_stride words apart (0: one for all); bit v % 32 of
+                                            word v / 32 is 1 where token v may be picked; NULL: every token may be            */
+  int64_t mask_stride;
+} csd_adjustment;                        /* Tokens outside of [0, V) count for nothing.  Logits and out aligned to their elements, the rest to
+                                            4 bytes; strides not negative, and rows of out must not overlap                   */
+int csd_adjust(const csd_adjustment* adjustment, void* stream);
 
 /* Waits for `stream` and copies the sticky CSD_STATUS_CAPACITY bit to *host_flags. */
 int csd_cache_status(csd_cache* cache, uint32_t* host_flags, void* stream);

@@ -119,7 +119,37 @@ struct MoveArgs {
   int64_t rows;
   int32_t n, Hk, groups;             // groups of eight of the n tokens
   uint32_t* status;
+  const int32_t* offsets;            // cache_write_packed(): rows + 1, of n tokens in all
 };
+
+// Sequences packed behind each other (offsets: count + 1), each in tiles of `wide` rows, `per` rows a token: sequence s begins at tile offset * per / wide
+// + s, which leaves room for all of its tiles and needs no sum over the sequences before it.  tokens * per / wide + count tiles
+// are in all; those behind the last of a sequence are empty.
+struct Sequence {
+  int32_t which, from, length;       // its first token, its tokens
+  int32_t tile;                      // of the sequence
+};
+__device__ inline Sequence sequence_of(const int32_t* offsets, int32_t count, int32_t tokens, uint32_t tile, uint32_t wide, uint32_t per) {
+  const auto offset = [&](int32_t s) {
+    const int32_t x = offsets[s];
+    return x < 0 ? 0 : x > tokens ? tokens : x;
+  };
+  const auto first = [&](int32_t from, int32_t s) { return (uint32_t)((uint64_t)from * per / wide) + (uint32_t)s; };
+  int32_t low = 0, high = count;     // the last sequence that begins at the tile or before it is in [low, high)
+  while (high - low > 1) {
+    const int32_t mid = (low + high) / 2;
+    if (first(offset(mid), mid) <= tile) low = mid;
+    else high = mid;
+  }
+  Sequence s;
+  s.which = low;
+  s.from = offset(low);
+  s.length = offset(low + 1) - s.from;
+  // (the tiles before the first sequence have none)
+  s.tile = (int32_t)(tile - first(s.from, low));
+  if (s.length < 0 || s.tile < 0) s.length = s.tile = 0;
+  return s;
+}
 
 // The shape of a call of csd_attend; every head_dim's kernels have a source of their own.
 struct AttendLaunch {
@@ -138,6 +168,12 @@ void attend_any(const AttendArgs& a, const AttendLaunch& how, int32_t head_dim, 
 int64_t parts_of_rows(int64_t rows, int32_t prompt_cap, int32_t path_cap);
 void cache_write(const MoveArgs& a, int32_t head_dim, bool f16, bool fp8, hipStream_t st);
 void cache_read(const MoveArgs& a, int32_t head_dim, bool f16, bool fp8, hipStream_t st);
+// csd_rotary's checks for heads of head_dim
+int check_rotary(const csd_rotary* how, int32_t head_dim);
+// move: keys and values, rows of n tokens each; H query heads
+void cache_write_rotated(const MoveArgs& move, const csd_rotary& how, const csd_heads& q, const int32_t* positions, int32_t H, void* q_out,
+                         int32_t head_dim, bool f16, bool fp8, hipStream_t st);
+void cache_write_packed(const MoveArgs& a, int32_t head_dim, bool f16, bool fp8, hipStream_t st);
 
 }  // namespace verify
 }  // namespace csd

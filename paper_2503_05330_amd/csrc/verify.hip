@@ -112,6 +112,7 @@ int move(csd_cache* c, bool read, bool prompt, int32_t layer, const csd_heads& k
   a.Hk = c->cfg.n_kv_heads;
   a.groups = (n + 7) / 8;
   a.status = c->status();
+  a.offsets = nullptr;
   if (read) cache_read(a, c->cfg.head_dim, c->cfg.type == CSD_F16, c->cfg.fp8, static_cast<hipStream_t>(stream));
   else cache_write(a, c->cfg.head_dim, c->cfg.type == CSD_F16, c->cfg.fp8, static_cast<hipStream_t>(stream));
   return finish(read ? "csd_cache_read" : "csd_cache_write");
@@ -191,6 +192,33 @@ int csd_cache_read(csd_cache* cache, int32_t layer, const int32_t* d_start, cons
 int csd_cache_read_prompt(csd_cache* cache, int32_t layer, const int32_t* d_start, const int32_t* d_counts, int32_t n, void* d_k,
                           void* d_v, void* stream) {
   return csd::verify::read(cache, true, layer, d_start, d_counts, n, d_k, d_v, stream);
+}
+
+int csd_cache_write_rotated(csd_cache* cache, int32_t layer, const csd_rotary* rotary, const csd_heads* q, const csd_heads* k, const csd_heads* v,
+                            const int32_t* d_positions, const int32_t* d_start, const int32_t* d_counts, int32_t n, void* d_q_out, void* stream) {
+  using namespace csd::verify;
+  if (check_move(cache, layer, n) != CSD_OK || check_rotary(rotary, cache->cfg.head_dim) != CSD_OK) return CSD_ERR_INVALID_ARG;
+  if (check_heads(q) != CSD_OK || check_heads(k) != CSD_OK || check_heads(v) != CSD_OK) return CSD_ERR_INVALID_ARG;
+  if (!d_positions || reinterpret_cast<uintptr_t>(d_positions) % 4 || !d_q_out || misaligned(d_q_out)) return CSD_ERR_INVALID_ARG;
+  const csd_cache_config& cfg = cache->cfg;
+  if ((int64_t)cfg.n_problems * cfg.n_paths * n > CSD_MAX_PACKED_TOKENS) return CSD_ERR_INVALID_ARG;
+  const MoveArgs a{cache->held(false, layer), *k, *v, d_start, d_counts, (int64_t)cfg.n_problems * cfg.n_paths, n, cfg.n_kv_heads, 0, cache->status(), nullptr};
+  cache_write_rotated(a, *rotary, *q, d_positions, cfg.n_heads, d_q_out, cfg.head_dim, cfg.type == CSD_F16, cfg.fp8, static_cast<hipStream_t>(stream));
+  return finish("csd_cache_write_rotated");
+}
+
+int csd_cache_write_packed(csd_cache* cache, int32_t layer, const csd_heads* k, const csd_heads* v, const int32_t* d_offsets, int64_t tokens,
+                           void* stream) {
+  using namespace csd::verify;
+  if (check_move(cache, layer, 1) != CSD_OK || tokens < 0 || tokens > CSD_MAX_PACKED_TOKENS) return CSD_ERR_INVALID_ARG;
+  if (!d_offsets || reinterpret_cast<uintptr_t>(d_offsets) % 4) return CSD_ERR_INVALID_ARG;
+  const csd_cache_config& cfg = cache->cfg;
+  if (cfg.n_problems > CSD_MAX_SEQUENCES) return CSD_ERR_INVALID_ARG;
+  if (tokens == 0) return CSD_OK;
+  if (check_heads(k) != CSD_OK || check_heads(v) != CSD_OK) return CSD_ERR_INVALID_ARG;
+  const MoveArgs a{cache->held(true, layer), *k, *v, nullptr, nullptr, cfg.n_problems, (int32_t)tokens, cfg.n_kv_heads, 0, cache->status(), d_offsets};
+  cache_write_packed(a, cfg.head_dim, cfg.type == CSD_F16, cfg.fp8, static_cast<hipStream_t>(stream));
+  return finish("csd_cache_write_packed");
 }
 
 int csd_attend(csd_cache* cache, int32_t layer, const csd_heads* q, const int32_t* d_prompt_len, const int32_t* d_path_len,

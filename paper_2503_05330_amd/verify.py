@@ -3,13 +3,16 @@
 Between Index.draft and Index.accept (binding.py) the target model sees every path's newest token and the draft
 behind it.  PathCache holds the keys and values of the prompts, which the paths of a problem share, and of the paths, in 16
 bits or quantised to 8 as they are written, and attends to them; targets() turns the logits into the tokens that
-Index.accept compares with, and the probabilities that Index.append and Index.step take.  Argument marshalling only, in
+Index.accept compares with, and the probabilities that Index.append and Index.step take.  Around these: rotate() and PathCache.write_rotated()
+turn queries and keys by their positions (Rotary), prompt_attend() is the prompts' own attention, which PathCache.write_packed()
+takes the keys and values of, and adjust() applies penalties, biases and masks to logits before targets().  Argument marshalling only, in
 native code (_csd_torch.so) where the arguments are the usual ones: all of it runs in the HIP kernels of libcsd.so, on the
 current stream.  Serving only: there are no gradients, and a tensor that requires one is refused unless gradients are off.
 """
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import Optional
 
 import torch
@@ -21,7 +24,8 @@ BF16, F16, F32 = 0, 1, 2
 TYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 
 EXPORTS = ["csd_cache_bytes", "csd_cache_create", "csd_cache_destroy", "csd_cache_write", "csd_cache_write_prompt",
-           "csd_cache_read", "csd_cache_read_prompt", "csd_attend", "csd_attend_form_of", "csd_targets_bytes", "csd_targets", "csd_cache_status"]
+           "csd_cache_read", "csd_cache_read_prompt", "csd_rotary_turns", "csd_rotate", "csd_cache_write_rotated", "csd_cache_write_packed",
+           "csd_prompt_attend", "csd_adjust", "csd_attend", "csd_attend_form_of", "csd_targets_bytes", "csd_targets", "csd_cache_status"]
 
 
 class CacheConfig(ctypes.Structure):
@@ -32,6 +36,18 @@ class CacheConfig(ctypes.Structure):
 
 class Heads(ctypes.Structure):
     _fields_ = [("data", _vp)] + [(name, ctypes.c_int64) for name in ("row_stride", "token_stride", "head_stride")]
+
+
+class RotaryConfig(ctypes.Structure):
+    _fields_ = [("turns", _vp), ("dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_float)]
+
+
+class Adjustment(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("n_problems", "n_paths", "n", "vocab", "type")] + [
+        ("logits", _vp), ("logit_stride", ctypes.c_int64), ("out", _vp), ("out_stride", ctypes.c_int64), ("counts", _vp), ("penalties", _vp),
+        ("tokens", _vp), ("token_stride", ctypes.c_int64), ("path_cap", ctypes.c_int32), ("path_len", _vp),
+        ("prompt", _vp), ("prompt_stride", ctypes.c_int64), ("prompt_cap", ctypes.c_int32), ("prompt_len", _vp),
+        ("bias", _vp), ("bias_stride", ctypes.c_int64), ("mask", _vp), ("mask_stride", ctypes.c_int64)]
 
 
 class AttendForm(ctypes.Structure):
@@ -56,6 +72,13 @@ def load() -> ctypes.CDLL:
             getattr(lib, name).argtypes = [_vp, i32, heads, heads, _vp, _vp, i32, _vp]
         for name in ("csd_cache_read", "csd_cache_read_prompt"):
             getattr(lib, name).argtypes = [_vp, i32, _vp, _vp, i32, _vp, _vp, _vp]
+        rotary, f64 = ctypes.POINTER(RotaryConfig), ctypes.c_double
+        lib.csd_rotary_turns.argtypes = [i32, f64, f64, f64, f64, f64, _vp]
+        lib.csd_rotate.argtypes = [rotary, heads, _vp, i64, i32, i32, i32, heads, _vp]
+        lib.csd_cache_write_rotated.argtypes = [_vp, i32, rotary, heads, heads, heads, _vp, _vp, _vp, i32, _vp, _vp]
+        lib.csd_cache_write_packed.argtypes = [_vp, i32, heads, heads, _vp, i64, _vp]
+        lib.csd_prompt_attend.argtypes = [heads, heads, heads, i32, i32, i32, i32, _vp, i32, i64, f32, _vp, _vp, _vp]
+        lib.csd_adjust.argtypes = [ctypes.POINTER(Adjustment), _vp]
         lib.csd_attend.argtypes = [_vp, i32, heads, _vp, _vp, _vp, i32, f32, i32, i32, _vp, _vp, _vp]
         lib.csd_attend_form_of.argtypes = [cfgp, i32, i32, i32, ctypes.POINTER(AttendForm)]
         lib.csd_targets_bytes.argtypes = [i64, i32, ctypes.POINTER(size)]
@@ -110,6 +133,30 @@ def attend_form(cfg: CacheConfig, n: int, prompt_bound: int = 0, path_bound: int
     form = AttendForm()
     _check(load().csd_attend_form_of(ctypes.byref(cfg), n, prompt_bound, path_bound, ctypes.byref(form)), "csd_attend_form_of")
     return form
+
+
+class Rotary:
+    """A rotation by position: the first dim values of a head in dim / 2 pairs, (i, i + dim / 2) or, interleaved, (2 i, 2 i + 1); pair i is
+    turned by position * base^(-2i/dim).  For longer contexts than a model was trained on these are divided by factor; with
+    original, the training's length, pairs of `high` turns over it and more stay, those of `low` turns and fewer are divided, and between
+    them a share is.  amplitude: what the pairs are multiplied by.  frequencies [dim / 2], in radians a token, instead of all that."""
+
+    def __init__(self, dim, base=10000.0, interleaved=False, factor=1.0, original=0, low=1.0, high=4.0, amplitude=1.0, frequencies=None,
+                 device="cuda"):
+        if frequencies is None:
+            turns = (ctypes.c_double * max(dim // 2, 1))()
+            _check(load().csd_rotary_turns(dim, base, factor, original, low, high, ctypes.addressof(turns)), "csd_rotary_turns")
+            turns = torch.tensor(list(turns), dtype=torch.float64)
+        else:
+            turns = torch.as_tensor(frequencies, dtype=torch.float64, device="cpu") / (2 * math.pi)
+            if turns.shape != (dim // 2,):
+                raise ValueError("%d frequencies, needs %d" % (turns.numel(), dim // 2))
+        if dim < 16 or dim % 16 or not math.isfinite(amplitude):
+            raise ValueError("a rotation of %d values, amplitude %g" % (dim, amplitude))
+        self.dim, self.interleaved, self.amplitude = dim, bool(interleaved), float(amplitude)
+        self.turns = turns.to(device)
+        self._cfg = RotaryConfig(self.turns.data_ptr(), dim, int(self.interleaved), self.amplitude)
+        self._native = (self._cfg.turns or 0, dim, self.interleaved, self.amplitude)
 
 
 class PathCache:
@@ -176,6 +223,33 @@ class PathCache:
         """k, v [P][n][kv heads][head_dim] to the prompts; start, counts [P]."""
         self._write(_lib.csd_cache_write_prompt, "csd_cache_write_prompt", (self.P,), layer, k, v, start, counts)
 
+    def write_rotated(self, layer, q, k, v, rotary, positions, start=None, counts=None):
+        """What rotate() does to q [P][N][n][heads][head_dim] and k at positions [P][N][n] int32, and write() with the rotated keys and v, in
+        one launch.  Returns the rotated queries, all n of each path."""
+        c, lead = self.cfg, (self.P, self.N)
+        rows = self.P * self.N
+        qh = _heads(q, self.dtype, lead, c.n_heads, c.head_dim)
+        kh, vh = (_heads(t, self.dtype, lead, c.n_kv_heads, c.head_dim) for t in (k, v))
+        n = q.shape[-3]
+        _here(q, k, v, rotary.turns, positions, start, counts)
+        if v.shape != k.shape or k.shape[-3] != n:
+            raise ValueError("queries of shape %s, keys of %s, values of %s" % (tuple(q.shape), tuple(k.shape), tuple(v.shape)))
+        out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        _check(load().csd_cache_write_rotated(self._h, layer, ctypes.byref(rotary._cfg), ctypes.byref(qh), ctypes.byref(kh), ctypes.byref(vh),
+                                              _ptr(positions, torch.int32, rows * n), _ptr(start, torch.int32, rows),
+                                              _ptr(counts, torch.int32, rows), n, out.data_ptr(), _stream()), "csd_cache_write_rotated")
+        return out
+
+    def write_packed(self, layer, k, v, offsets):
+        """k, v [tokens][kv heads][head_dim] of all prompts behind each other: problem p's are offsets[p] .. offsets[p + 1] - 1 (offsets [P + 1]
+        int32, ascending), which become its prompt, from position 0 on."""
+        c = self.cfg
+        kh, vh = (_packed(t, self.dtype, c.n_kv_heads, c.head_dim) for t in (k, v))
+        if v.shape != k.shape:
+            raise ValueError("keys of shape %s, values of shape %s" % (tuple(k.shape), tuple(v.shape)))
+        _check(load().csd_cache_write_packed(self._h, layer, ctypes.byref(kh), ctypes.byref(vh), _ptr(offsets, torch.int32, self.P + 1),
+                                             len(k), _stream()), "csd_cache_write_packed")
+
     def _read(self, call, what, lead, layer, n, start, counts):
         got = _native.cache_read(*self._cache(), len(lead) == 1, layer, n, start, counts)
         if got is not None:
@@ -227,6 +301,133 @@ class PathCache:
         flags = ctypes.c_uint32(0)
         _check(load().csd_cache_status(self._h, ctypes.byref(flags), _stream()), "csd_cache_status")
         return flags.value
+
+
+def _here(*tensors) -> None:
+    """The launches are of the current device."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
+            raise ValueError("a tensor of cuda:%d while cuda:%d is the current device" % (t.get_device(), torch._C._cuda_getDevice()))
+
+
+def _packed(t: torch.Tensor, dtype, n_heads: int, dim: int) -> Heads:
+    """A tensor [tokens][heads][dim], or one with several evenly spaced leading axes of tokens."""
+    if not t.is_cuda or t.dtype != dtype:
+        raise TypeError("expected a device tensor of dtype %s" % dtype)
+    _here(t)
+    _no_gradients(t)
+    shape, stride = tuple(t.shape), t.stride()
+    if len(shape) < 3 or shape[-2:] != (n_heads, dim):
+        raise ValueError("tensor of shape %s, needs %s" % (shape, ("tokens", n_heads, dim)))
+    if stride[-1] != 1:
+        raise TypeError("a head's values must be contiguous")
+    h = Heads(t.data_ptr(), 0, _spacing(shape[:-2], stride), stride[-2] if n_heads > 1 else 0)
+    if (h.data or 0) % 16 or h.token_stride % 8 or h.head_stride % 8:
+        raise ValueError("heads must start at multiples of 16 bytes")
+    return h
+
+
+def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
+    ends = lambda t: (t.data_ptr(), t.data_ptr() + (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) * t.element_size())
+    (x, y), (z, w) = ends(a), ends(b)
+    return a.numel() > 0 and b.numel() > 0 and x < w and z < y
+
+
+def rotate(x: torch.Tensor, positions: torch.Tensor, rotary: Rotary, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Queries and keys x [..., heads, head_dim] (bfloat16, float16; a slice of a projection's output is fine) turned by their positions
+    [...] int32: the first rotary.dim values of each head, the others as they are.  out: x itself, or another tensor of its shape."""
+    if x.dim() < 3 or x.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("expected [..., heads, head_dim] of bfloat16 or float16")
+    if positions.shape != x.shape[:-2]:
+        raise ValueError("positions of shape %s, needs %s" % (tuple(positions.shape), tuple(x.shape[:-2])))
+    H, D = x.shape[-2:]
+    heads = _packed(x, x.dtype, H, D)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    elif out.shape != x.shape:
+        raise ValueError("out of shape %s, needs %s" % (tuple(out.shape), tuple(x.shape)))
+    to = _packed(out, x.dtype, H, D)
+    _here(positions, rotary.turns)
+    if _overlap(x, out) and (x.data_ptr() != out.data_ptr() or x.stride() != out.stride()):
+        raise ValueError("out overlaps x")
+    _check(load().csd_rotate(ctypes.byref(rotary._cfg), ctypes.byref(heads), _ptr(positions, torch.int32, positions.numel()), positions.numel(),
+                             H, D, TYPES[x.dtype], ctypes.byref(to), _stream()), "csd_rotate")
+    return out
+
+
+def prompt_attend(q, k, v, offsets, scale=None, out=None, lse=None):
+    """Attention of packed sequences to themselves: q [tokens][heads][head_dim], k, v [tokens][kv heads][head_dim] (bfloat16, float16; slices of a
+    projection's output are fine), sequence s the tokens offsets[s] .. offsets[s + 1] - 1 (offsets int32, ascending), each of which sees
+    those up to itself.  Returns [tokens][heads][head_dim]; lse: a float32 tensor [tokens][heads] that takes the logarithms of the sums.
+    scale: 1 / sqrt(head_dim) where None.  Tokens of no sequence are not written (where out is None they hold anything)."""
+    if q.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16) or k.dim() != 3:
+        raise TypeError("expected [tokens][heads][head_dim] of bfloat16 or float16")
+    n, H, D = q.shape
+    Hk = k.shape[1]
+    heads = _packed(q, q.dtype, H, D), _packed(k, q.dtype, Hk, D), _packed(v, q.dtype, Hk, D)
+    if len(k) != n or v.shape != k.shape:
+        raise ValueError("queries of shape %s, keys of %s, values of %s" % (tuple(q.shape), tuple(k.shape), tuple(v.shape)))
+    _no_gradients(out, lse)
+    _here(out, lse, offsets)
+    if out is None:
+        out = torch.empty((n, H, D), dtype=q.dtype, device=q.device)
+    if offsets.dim() != 1 or len(offsets) < 2:
+        raise ValueError("offsets of shape %s" % (tuple(offsets.shape),))
+    if any(_overlap(out, t) for t in (q, k, v)):
+        raise ValueError("out overlaps an input")
+    _check(load().csd_prompt_attend(*map(ctypes.byref, heads), TYPES[q.dtype], H, Hk, D, _ptr(offsets, torch.int32), len(offsets) - 1, n,
+                                    D ** -0.5 if scale is None else scale, _ptr(out, q.dtype, n * H * D), _ptr(lse, torch.float32, n * H),
+                                    _stream()), "csd_prompt_attend")
+    return out
+
+
+def adjust(logits, tokens=None, path_len=None, counts=None, prompt=None, prompt_len=None, penalties=None, bias=None, mask=None, out=None):
+    """Logits [P][N][n][vocab] (bfloat16, float16, float32) as they are sampled from, before targets().  Position t of a path has said the first path_len
+    - counts + t + 1 of its tokens [P][N][any] int32 (path_len, counts [P][N] int32, as in attend(); counts None: n), and its prompt's first
+    prompt_len [P] (None: all) of prompt [P][any].  penalties [P][3] float32, repetition, presence and frequency: the logit of a token that
+    was said is divided by repetition where positive, else multiplied; one that the path said c times loses frequency * c + presence.
+    bias [P][vocab] or [vocab] float32 is added.  mask [P][N][n][words] or [words] int32: bit v % 32 of word v / 32 is 0
+    where token v becomes -inf.  Positions beyond a path's count become zeros.  out: logits itself, or another tensor of its shape."""
+    if logits.dtype not in TYPES or logits.dim() != 4:
+        raise TypeError("expected logits [P][N][n][vocab]")
+    _no_gradients(logits, penalties, bias, out)
+    _here(logits, tokens, path_len, counts, prompt, prompt_len, penalties, bias, mask, out)
+    P, N, n, V = logits.shape
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    if out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out of shape %s and type %s" % (tuple(out.shape), out.dtype))
+
+    def rows(t, dtype, lead, what):
+        """(address, distance of the rows, row length) of [*lead][any]"""
+        if t is None:
+            return None, 0, 0
+        if not t.is_cuda or t.dtype != dtype:
+            raise TypeError("expected %s as a device tensor of dtype %s" % (what, dtype))
+        if t.dim() != len(lead) + 1 or tuple(t.shape[:-1]) != tuple(lead) or (t.stride(-1) != 1 and t.shape[-1] > 1):
+            raise ValueError("%s of shape %s, needs rows %s" % (what, tuple(t.shape), tuple(lead)))
+        return t.data_ptr(), _spacing(t.shape[:-1], t.stride()), t.shape[-1]
+    x, x_stride, _ = rows(logits, logits.dtype, (P, N, n), "logits")
+    y, y_stride, _ = rows(out, logits.dtype, (P, N, n), "out")
+    if _overlap(logits, out) and (x != y or logits.stride() != out.stride()):
+        raise ValueError("out overlaps the logits")
+    said, said_stride, path_cap = rows(tokens, torch.int32, (P, N), "tokens")
+    asked, asked_stride, prompt_cap = rows(prompt, torch.int32, (P,), "prompt")
+    b, b_stride, b_size = rows(bias, torch.float32, () if bias is not None and bias.dim() == 1 else (P,), "bias")
+    m, m_stride, m_size = rows(mask, torch.int32, () if mask is not None and mask.dim() == 1 else (P, N, n), "mask")
+    if (bias is not None and b_size != V) or (mask is not None and m_size < (V + 31) // 32):
+        raise ValueError("bias or mask too short for %d tokens" % V)
+    if tokens is not None and path_len is None:
+        raise ValueError("tokens need path_len")
+    if tokens is not None and path_cap == 0:
+        said = None
+    if prompt is not None and prompt_cap == 0:
+        asked = None
+    a = Adjustment(P, N, n, V, TYPES[logits.dtype], x, x_stride, y, y_stride, _ptr(counts, torch.int32, P * N), _ptr(penalties, torch.float32, 3 * P),
+                   said, said_stride, path_cap, _ptr(path_len, torch.int32, P * N), asked, asked_stride, prompt_cap,
+                   _ptr(prompt_len, torch.int32, P), b, b_stride, m, m_stride)
+    _check(load().csd_adjust(ctypes.byref(a), _stream()), "csd_adjust")
+    return out
 
 
 def targets(logits: torch.Tensor, noise: Optional[torch.Tensor] = None, inv_temperature: float = 1.0):
