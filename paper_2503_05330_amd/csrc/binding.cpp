@@ -467,6 +467,235 @@ PyObject* targets(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// The stream, the current device, which every tensor has to be of, and a rotation (verify.Rotary): arguments of the calls below.
+struct Device {
+  void* stream;
+  int64_t index;
+  explicit Device(Call& c) : stream(c.pointer()), index(c.integer()) {
+    if (index < 0 || index > 127) c.usual = false;
+  }
+  c10::Device device() const { return c10::Device(c10::DeviceType::CUDA, (c10::DeviceIndex)index); }
+  void holds(Call& c, const at::Tensor* t) const {
+    if (t && t->get_device() != index) c.usual = false;
+  }
+};
+struct Rotation {
+  csd_rotary how;
+  Rotation(Call& c, const Device& d) {
+    how.d_turns = static_cast<const double*>(c.pointer());
+    how.dim = c.small();
+    how.interleaved = c.truth();
+    how.amplitude = c.real();
+    if (c.integer() != d.index) c.usual = false;
+  }
+};
+
+// Tokens [..., heads, D] of `type`, the leading axes evenly spaced; *n is set where it is below 0, and has to be the tensor's tokens where not.
+csd_heads packed_of(Call& c, const Device& d, at::ScalarType type, int64_t heads, int64_t D, int64_t* n, const at::Tensor** of = nullptr) {
+  const at::Tensor* t = c.any_tensor();
+  if (!t || t->dim() < 3 || t->scalar_type() != type) {
+    c.usual = false;
+    return csd_heads{};
+  }
+  d.holds(c, t);
+  const auto sizes = t->sizes(), strides = t->strides();
+  const int64_t axes = t->dim() - 2;
+  int64_t tokens = 1;
+  for (int64_t i = 0; i < axes; ++i) tokens *= sizes[i];
+  if (*n < 0) *n = tokens;
+  if (tokens != *n || tokens == 0 || sizes[axes] != heads || sizes[axes + 1] != D || strides[axes + 1] != 1) c.usual = false;
+  const csd_heads h{t->data_ptr(), 0, spacing(c, sizes, strides, axes), heads > 1 ? strides[axes] : 0};
+  if (reinterpret_cast<uintptr_t>(h.data) % 16 || h.token_stride % 8 || h.head_stride % 8) c.usual = false;
+  if (of) *of = t;
+  return h;
+}
+// contiguous, of exactly these many numbers
+const int32_t* ints_of(Call& c, const Device& d, int64_t numel, bool maybe) {
+  const at::Tensor* t = c.any_tensor(maybe);
+  if (!t) return nullptr;
+  d.holds(c, t);
+  if (t->scalar_type() != at::kInt || !t->is_contiguous() || t->numel() < numel) c.usual = false;
+  return static_cast<const int32_t*>(t->data_ptr());
+}
+
+// the sizes of the tensor that comes next, which stays the next; its type
+const at::Tensor* peek(const Call& c, int64_t at_least) {
+  if (c.at >= c.n || !THPVariable_CheckExact(c.args[c.at])) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(c.args[c.at]);
+  return t.dim() >= at_least ? &t : nullptr;
+}
+
+// rotate(stream, device, rotation, x, positions): (code, result)
+PyObject* rotate(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  Call c{args, n_args};
+  const Device d(c);
+  const Rotation r(c, d);
+  const at::Tensor* x = peek(c, 3);
+  if (!x || !c.usual || (x->scalar_type() != at::kBFloat16 && x->scalar_type() != at::kHalf)) Py_RETURN_NONE;
+  const auto sizes = x->sizes();
+  const int64_t H = sizes[x->dim() - 2], D = sizes[x->dim() - 1];
+  int64_t n = -1;
+  const csd_heads from = packed_of(c, d, x->scalar_type(), H, D, &n);
+  const at::Tensor* positions = peek(c, 1);
+  const int32_t* at = ints_of(c, d, n, false);
+  if (!c.usual || !positions || positions->sizes() != sizes.slice(0, x->dim() - 2) || H > INT32_MAX || D > INT32_MAX) Py_RETURN_NONE;
+  Maker make(d.device());
+  const at::Tensor out = make(x->scalar_type(), sizes);
+  const csd_heads to{out.data_ptr(), 0, H * D, D};
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = csd_rotate(&r.how, &from, at, n, (int32_t)H, (int32_t)D, x->scalar_type() == at::kHalf ? CSD_F16 : CSD_BF16, &to, d.stream);
+  Py_END_ALLOW_THREADS
+  return Py_BuildValue("(iN)", code, THPVariable_Wrap(out));
+  END_HANDLE_TH_ERRORS
+}
+
+// cache_write_rotated(cache, stream, device, rotation, layer, q, k, v, positions, start, counts): (code, queries)
+PyObject* cache_write_rotated(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  Call c{args, n_args};
+  const Cache x(c);
+  const Device d(c);
+  const Rotation r(c, d);
+  const int32_t layer = c.small();
+  int64_t n = 0;
+  for (int i = 0; i < 3; ++i)
+    if (c.at + i < c.n && THPVariable_CheckExact(c.args[c.at + i])) d.holds(c, &THPVariable_Unpack(c.args[c.at + i]));
+  const csd_heads q = heads_of(c, x, x.N, x.H, &n), k = heads_of(c, x, x.N, x.Hk, &n), v = heads_of(c, x, x.N, x.Hk, &n);
+  const int64_t rows = x.P * x.N;
+  const int32_t* at = ints_of(c, d, rows * n, false);
+  const int32_t *start = ints_of(c, d, rows, true), *counts = ints_of(c, d, rows, true);
+  if (!c.usual) Py_RETURN_NONE;
+  const int64_t sizes[] = {x.P, x.N, n, x.H, x.D};
+  Maker make(d.device());
+  const at::Tensor out = make(x.type, c10::IntArrayRef(sizes, 5));
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = csd_cache_write_rotated(x.handle, layer, &r.how, &q, &k, &v, at, start, counts, (int32_t)n, out.data_ptr(), d.stream);
+  Py_END_ALLOW_THREADS
+  return Py_BuildValue("(iN)", code, THPVariable_Wrap(out));
+  END_HANDLE_TH_ERRORS
+}
+
+// prompt_attend(stream, device, q, k, v, offsets, scale): (code, result)
+PyObject* prompt_attend(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  Call c{args, n_args};
+  const Device d(c);
+  const at::Tensor* x = peek(c, 3);
+  if (!x || !c.usual || x->dim() != 3 || (x->scalar_type() != at::kBFloat16 && x->scalar_type() != at::kHalf)) Py_RETURN_NONE;
+  const at::ScalarType type = x->scalar_type();
+  const int64_t H = x->size(1), D = x->size(2);
+  int64_t n = -1;
+  const csd_heads q = packed_of(c, d, type, H, D, &n);
+  const at::Tensor* y = peek(c, 3);
+  if (!y || y->dim() != 3) Py_RETURN_NONE;
+  const int64_t Hk = y->size(1);
+  const csd_heads k = packed_of(c, d, type, Hk, D, &n);
+  const at::Tensor* z = peek(c, 3);
+  if (!z || z->dim() != 3) Py_RETURN_NONE;
+  const csd_heads v = packed_of(c, d, type, Hk, D, &n);
+  const at::Tensor* o = peek(c, 1);
+  const int32_t* offsets = ints_of(c, d, 2, false);
+  const float scale = c.real();
+  if (!c.usual || !o || o->dim() != 1 || o->numel() - 1 > INT32_MAX || H > INT32_MAX || Hk > INT32_MAX || D > INT32_MAX) Py_RETURN_NONE;
+  const int64_t sizes[] = {n, H, D};
+  Maker make(d.device());
+  const at::Tensor out = make(type, c10::IntArrayRef(sizes, 3));
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = csd_prompt_attend(&q, &k, &v, type == at::kHalf ? CSD_F16 : CSD_BF16, (int32_t)H, (int32_t)Hk, (int32_t)D, offsets, (int32_t)(o->numel() - 1), n, scale,
+                           out.data_ptr(), nullptr, d.stream);
+  Py_END_ALLOW_THREADS
+  return Py_BuildValue("(iN)", code, THPVariable_Wrap(out));
+  END_HANDLE_TH_ERRORS
+}
+
+// Rows [lead][any] of a type, or None: address, distance of the rows, row length.
+struct RowsOf {
+  void* data = nullptr;
+  int64_t stride = 0, size = 0;
+  RowsOf(Call& c, const Device& d, at::ScalarType type, const c10::IntArrayRef lead, bool shared) {
+    const at::Tensor* t = c.any_tensor(true);
+    if (!t) return;
+    d.holds(c, t);
+    const int64_t axes = t->dim() - 1;
+    if (t->scalar_type() != type || axes < 0 || !((shared && axes == 0) || t->sizes().slice(0, axes) == lead) || t->strides()[axes] != 1) {
+      c.usual = false;
+      return;
+    }
+    data = t->data_ptr();
+    stride = spacing(c, t->sizes(), t->strides(), axes);
+    size = t->size(axes);
+    if (size == 0 || size > INT32_MAX) c.usual = false;
+  }
+};
+
+// adjust(stream, device, logits, tokens, path_len, counts, prompt, prompt_len, penalties, bias, mask, out): (code, result)
+PyObject* adjust(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  Call c{args, n_args};
+  const Device d(c);
+  PyObject* const given = c.at < c.n ? c.args[c.at] : Py_None;
+  const at::Tensor* x = c.any_tensor();
+  if (!c.usual || x->dim() != 4) Py_RETURN_NONE;
+  d.holds(c, x);
+  const auto sizes = x->sizes(), strides = x->strides();
+  const at::ScalarType type = x->scalar_type();
+  const int32_t of_type = type == at::kBFloat16 ? CSD_BF16 : type == at::kHalf ? CSD_F16 : type == at::kFloat ? CSD_F32 : -1;
+  const int64_t P = sizes[0], N = sizes[1], n = sizes[2], V = sizes[3], rows = P * N;
+  if (of_type < 0 || strides[3] != 1 || P <= 0 || N <= 0 || n <= 0 || V <= 0 || P > INT32_MAX || N > INT32_MAX || n > INT32_MAX || V > INT32_MAX) Py_RETURN_NONE;
+  csd_adjustment a{};
+  a.n_problems = (int32_t)P;
+  a.n_paths = (int32_t)N;
+  a.n = (int32_t)n;
+  a.vocab = (int32_t)V;
+  a.type = of_type;
+  a.d_logits = x->data_ptr();
+  a.logit_stride = spacing(c, sizes, strides, 3);
+  const RowsOf tokens(c, d, at::kInt, sizes.slice(0, 2), false);
+  a.d_path_len = ints_of(c, d, rows, !tokens.data);
+  a.d_counts = ints_of(c, d, rows, true);
+  const RowsOf prompt(c, d, at::kInt, sizes.slice(0, 1), false);
+  a.d_prompt_len = ints_of(c, d, P, true);
+  const at::Tensor* penalties = c.any_tensor(true);
+  if (penalties) {
+    d.holds(c, penalties);
+    if (penalties->scalar_type() != at::kFloat || !penalties->is_contiguous() || penalties->numel() < 3 * P) c.usual = false;
+    a.d_penalties = static_cast<const float*>(penalties->data_ptr());
+  }
+  const RowsOf bias(c, d, at::kFloat, sizes.slice(0, 1), true), mask(c, d, at::kInt, sizes.slice(0, 3), true);
+  PyObject* const out = c.next();
+  if (!c.usual || (out != Py_None && out != given) || (bias.data && bias.size != V) || (mask.data && mask.size < (V + 31) / 32)) Py_RETURN_NONE;
+  a.d_tokens = static_cast<const int32_t*>(tokens.data);
+  a.token_stride = tokens.stride;
+  a.path_cap = (int32_t)tokens.size;
+  a.d_prompt = static_cast<const int32_t*>(prompt.data);
+  a.prompt_stride = prompt.stride;
+  a.prompt_cap = (int32_t)prompt.size;
+  a.d_bias = static_cast<const float*>(bias.data);
+  a.bias_stride = bias.stride;
+  a.d_mask = static_cast<const uint32_t*>(mask.data);
+  a.mask_stride = mask.stride;
+  at::Tensor made;
+  a.d_out = const_cast<void*>(a.d_logits);
+  a.out_stride = a.logit_stride;
+  if (out == Py_None) {
+    Maker make(d.device());
+    made = make(type, sizes);
+    a.d_out = made.data_ptr();
+    a.out_stride = V;
+  }
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = csd_adjust(&a, d.stream);
+  Py_END_ALLOW_THREADS
+  if (made.defined()) return Py_BuildValue("(iN)", code, THPVariable_Wrap(made));
+  return Py_BuildValue("(iO)", code, given);
+  END_HANDLE_TH_ERRORS
+}
+
 template <class F>
 PyCFunction fast(F f) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(f));
@@ -482,6 +711,10 @@ PyMethodDef methods[] = {
     {"cache_read", fast(cache_read), METH_FASTCALL, nullptr},
     {"attend", fast(attend), METH_FASTCALL, nullptr},
     {"targets", fast(targets), METH_FASTCALL, nullptr},
+    {"rotate", fast(rotate), METH_FASTCALL, nullptr},
+    {"cache_write_rotated", fast(cache_write_rotated), METH_FASTCALL, nullptr},
+    {"prompt_attend", fast(prompt_attend), METH_FASTCALL, nullptr},
+    {"adjust", fast(adjust), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_csd_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -156,7 +156,14 @@ class Rotary:
         self.dim, self.interleaved, self.amplitude = dim, bool(interleaved), float(amplitude)
         self.turns = turns.to(device)
         self._cfg = RotaryConfig(self.turns.data_ptr(), dim, int(self.interleaved), self.amplitude)
-        self._native = (self._cfg.turns or 0, dim, self.interleaved, self.amplitude)
+        # what every native call starts with
+        self._call = self._cfg.turns or 0, dim, self.interleaved, self.amplitude, self.turns.get_device()
+
+    def _config(self):
+        if not self.turns.is_cuda:
+            raise TypeError("a rotation whose turns are not on the device")
+        _here(self.turns)
+        return ctypes.byref(self._cfg)
 
 
 class PathCache:
@@ -226,16 +233,20 @@ class PathCache:
     def write_rotated(self, layer, q, k, v, rotary, positions, start=None, counts=None):
         """What rotate() does to q [P][N][n][heads][head_dim] and k at positions [P][N][n] int32, and write() with the rotated keys and v, in
         one launch.  Returns the rotated queries, all n of each path."""
+        got = _native.cache_write_rotated(*self._cache(), *_now(), *rotary._call, layer, q, k, v, positions, start, counts)
+        if got is not None:
+            _check(got[0], "csd_cache_write_rotated")
+            return got[1]
         c, lead = self.cfg, (self.P, self.N)
         rows = self.P * self.N
         qh = _heads(q, self.dtype, lead, c.n_heads, c.head_dim)
         kh, vh = (_heads(t, self.dtype, lead, c.n_kv_heads, c.head_dim) for t in (k, v))
         n = q.shape[-3]
-        _here(q, k, v, rotary.turns, positions, start, counts)
+        _here(q, k, v, positions, start, counts)
         if v.shape != k.shape or k.shape[-3] != n:
             raise ValueError("queries of shape %s, keys of %s, values of %s" % (tuple(q.shape), tuple(k.shape), tuple(v.shape)))
         out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-        _check(load().csd_cache_write_rotated(self._h, layer, ctypes.byref(rotary._cfg), ctypes.byref(qh), ctypes.byref(kh), ctypes.byref(vh),
+        _check(load().csd_cache_write_rotated(self._h, layer, rotary._config(), ctypes.byref(qh), ctypes.byref(kh), ctypes.byref(vh),
                                               _ptr(positions, torch.int32, rows * n), _ptr(start, torch.int32, rows),
                                               _ptr(counts, torch.int32, rows), n, out.data_ptr(), _stream()), "csd_cache_write_rotated")
         return out
@@ -310,6 +321,11 @@ def _here(*tensors) -> None:
             raise ValueError("a tensor of cuda:%d while cuda:%d is the current device" % (t.get_device(), torch._C._cuda_getDevice()))
 
 
+def _now():
+    """The current stream and device."""
+    return _stream(), torch._C._cuda_getDevice()
+
+
 def _packed(t: torch.Tensor, dtype, n_heads: int, dim: int) -> Heads:
     """A tensor [tokens][heads][dim], or one with several evenly spaced leading axes of tokens."""
     if not t.is_cuda or t.dtype != dtype:
@@ -336,6 +352,12 @@ def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
 def rotate(x: torch.Tensor, positions: torch.Tensor, rotary: Rotary, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Queries and keys x [..., heads, head_dim] (bfloat16, float16; a slice of a projection's output is fine) turned by their positions
     [...] int32: the first rotary.dim values of each head, the others as they are.  out: x itself, or another tensor of its shape."""
+    if out is None and x.is_cuda:
+        load()
+        got = _native.rotate(*_now(), *rotary._call, x, positions)
+        if got is not None:
+            _check(got[0], "csd_rotate")
+            return got[1]
     if x.dim() < 3 or x.dtype not in (torch.bfloat16, torch.float16):
         raise TypeError("expected [..., heads, head_dim] of bfloat16 or float16")
     if positions.shape != x.shape[:-2]:
@@ -347,10 +369,10 @@ def rotate(x: torch.Tensor, positions: torch.Tensor, rotary: Rotary, out: Option
     elif out.shape != x.shape:
         raise ValueError("out of shape %s, needs %s" % (tuple(out.shape), tuple(x.shape)))
     to = _packed(out, x.dtype, H, D)
-    _here(positions, rotary.turns)
+    _here(positions)
     if _overlap(x, out) and (x.data_ptr() != out.data_ptr() or x.stride() != out.stride()):
         raise ValueError("out overlaps x")
-    _check(load().csd_rotate(ctypes.byref(rotary._cfg), ctypes.byref(heads), _ptr(positions, torch.int32, positions.numel()), positions.numel(),
+    _check(load().csd_rotate(rotary._config(), ctypes.byref(heads), _ptr(positions, torch.int32, positions.numel()), positions.numel(),
                              H, D, TYPES[x.dtype], ctypes.byref(to), _stream()), "csd_rotate")
     return out
 
@@ -360,6 +382,12 @@ def prompt_attend(q, k, v, offsets, scale=None, out=None, lse=None):
     projection's output are fine), sequence s the tokens offsets[s] .. offsets[s + 1] - 1 (offsets int32, ascending), each of which sees
     those up to itself.  Returns [tokens][heads][head_dim]; lse: a float32 tensor [tokens][heads] that takes the logarithms of the sums.
     scale: 1 / sqrt(head_dim) where None.  Tokens of no sequence are not written (where out is None they hold anything)."""
+    if out is None and lse is None and q.is_cuda and q.dim() == 3:
+        load()
+        got = _native.prompt_attend(*_now(), q, k, v, offsets, q.shape[-1] ** -0.5 if scale is None else scale)
+        if got is not None:
+            _check(got[0], "csd_prompt_attend")
+            return got[1]
     if q.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16) or k.dim() != 3:
         raise TypeError("expected [tokens][heads][head_dim] of bfloat16 or float16")
     n, H, D = q.shape
@@ -388,6 +416,12 @@ def adjust(logits, tokens=None, path_len=None, counts=None, prompt=None, prompt_
     was said is divided by repetition where positive, else multiplied; one that the path said c times loses frequency * c + presence.
     bias [P][vocab] or [vocab] float32 is added.  mask [P][N][n][words] or [words] int32: bit v % 32 of word v / 32 is 0
     where token v becomes -inf.  Positions beyond a path's count become zeros.  out: logits itself, or another tensor of its shape."""
+    if logits.is_cuda:
+        load()
+        got = _native.adjust(*_now(), logits, tokens, path_len, counts, prompt, prompt_len, penalties, bias, mask, out)
+        if got is not None:
+            _check(got[0], "csd_adjust")
+            return got[1]
     if logits.dtype not in TYPES or logits.dim() != 4:
         raise TypeError("expected logits [P][N][n][vocab]")
     _no_gradients(logits, penalties, bias, out)

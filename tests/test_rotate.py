@@ -190,6 +190,7 @@ def test_arguments_that_are_refused(gen):
         (lambda: verify.rotate(x, at, rotary, out=x[:, :3]), ValueError), (lambda: verify.rotate(x, at, rotary, out=x.flip(0)[:, :2]), ValueError),
         (lambda: verify.rotate(x[:5], at[:5], rotary, out=x[1:]), ValueError), (lambda: verify.rotate(wants(x), at, rotary), TypeError),
         (lambda: verify.rotate(x, at, rotary, out=wants(x)), TypeError), (lambda: verify.rotate(x[..., 1:57], at, verify.Rotary(16)), ValueError),
+        (lambda: verify.rotate(x, at, verify.Rotary(64, device="cpu")), TypeError),
     ]:
         with pytest.raises(error):
             call()
@@ -201,6 +202,7 @@ def test_arguments_that_are_refused(gen):
         (lambda: c.write_rotated(1, q, k, k, rotary, at), binding.CsdError), (lambda: c.write_rotated(0, q, k, k, verify.Rotary(128), at), binding.CsdError),
         (lambda: c.write_rotated(0, q.half(), k, k, rotary, at), TypeError), (lambda: c.write_rotated(0, q, wants(k), k, rotary, at), TypeError),
         (lambda: c.write_rotated(0, q, k, k, rotary, at, ints([1])), ValueError),
+        (lambda: c.write_rotated(0, q, k, k, verify.Rotary(64, device="cpu"), at), TypeError),
     ]:
         with pytest.raises(error):
             call()
