@@ -2,7 +2,6 @@
 #pragma once
 
 #include "csd_attend_rows.cuh"
-#include "csd_launch.h"
 
 namespace csd {
 namespace verify {

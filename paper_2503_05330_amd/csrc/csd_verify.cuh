@@ -16,6 +16,9 @@
 #include "csd_verify.h"
 
 namespace csd {
+
+int hip_fail(hipError_t e, const char* what);          // keeps the text that csd_strerror gives for CSD_ERR_HIP, which it returns
+
 namespace verify {
 
 constexpr int kBlock = 32;              // tokens of a block

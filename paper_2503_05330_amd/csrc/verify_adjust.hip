@@ -4,7 +4,6 @@
 // stretch is counted in LDS once: bits 0 .. 29 of a token's word count what the path said before its newest tokens, bit 30 says that one
 // of these is the token (then they are looked through up to the row's position), bit 31 that the prompt has it.  Most words are zero: such
 // logits are copied, with their bias and bit of the mask.
-#include "csd_launch.h"
 #include "csd_verify.cuh"
 
 namespace csd {
@@ -13,10 +12,46 @@ namespace {
 
 constexpr uint32_t kNew = 1u << 30, kPrompt = 1u << 31;
 
+constexpr int kThreads = 512;
+
+// Tokens that the workgroup looks at: the first few of each thread are asked for at once, so that they are on their way together with all else.
+struct Tokens {
+  typedef int32_t Four __attribute__((ext_vector_type(4), aligned(4)));
+  static constexpr int kAhead = 3;
+  const int32_t* from;
+  int32_t length;
+  Four first[kAhead];
+  __device__ void ask(Four (&x)[kAhead], int32_t x0) const {
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+      const int32_t at = x0 + s * kThreads;
+      x[s] = 4 * at + 3 < length ? *reinterpret_cast<const Four*>(from + 4 * at) : Four{};
+    }
+  }
+  __device__ Tokens(const int32_t* from, int32_t length) : from(from), length(length) { ask(first, threadIdx.x); }
+  // calls f with each
+  template <class F>
+  __device__ void each(F f) const {
+    const int32_t fours = length / 4;
+    Four x[kAhead];
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) x[s] = first[s];
+    for (int32_t x0 = threadIdx.x; x0 < fours; x0 += kAhead * kThreads) {
+      if (x0 != (int32_t)threadIdx.x) ask(x, x0);
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) {
+        if (x0 + s * kThreads >= fours) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f((uint32_t)x[s][i]);
+      }
+    }
+    if ((int32_t)threadIdx.x < length - 4 * fours) f((uint32_t)from[4 * fours + threadIdx.x]);
+  }
+};
+
 template <class E>
-__global__ __launch_bounds__(512) void adjust_kernel(csd_adjustment a, int32_t first_path, int32_t parts, int32_t per) {
-  constexpr int kThreads = 512;
-  extern __shared__ uint32_t words[];                    // of the stretch's tokens
+__global__ __launch_bounds__(kThreads) void adjust_kernel(csd_adjustment a, int32_t first_path, int32_t parts, int32_t per) {
+  extern __shared__ __align__(32) uint32_t words[];      // of the stretch's tokens
   __shared__ int32_t newest[CSD_MAX_VERIFY_STEP];
   const int32_t path = first_path + blockIdx.x / (uint32_t)parts, part = blockIdx.x % (uint32_t)parts, p = path / a.n_paths;
   const int32_t from = part * per, size = a.vocab - from < per ? a.vocab - from : per;
@@ -24,73 +59,122 @@ __global__ __launch_bounds__(512) void adjust_kernel(csd_adjustment a, int32_t f
   count = count < 0 ? 0 : count > a.n ? a.n : count;
   const bool penalties = a.d_penalties != nullptr;
   float repetition = 1, presence = 0, frequency = 0;
-  int32_t before = 0, path_len = 0;                      // tokens before the newest ones; the newest: before .. before + count - 1, where they are there
+  int32_t before = 0;                                    // tokens before the newest ones, which are before .. before + count - 1, where they are there
+  const int32_t* said = nullptr;
+  if (penalties && count && a.d_tokens) {
+    int32_t path_len = a.d_path_len[path];
+    path_len = path_len < 0 ? 0 : path_len > a.path_cap ? a.path_cap : path_len;
+    before = path_len - count;
+    said = a.d_tokens + path * a.token_stride;
+  }
+  int32_t length = 0;
+  if (penalties && count && a.d_prompt) {
+    length = a.d_prompt_len ? a.d_prompt_len[p] : a.prompt_cap;
+    length = length < 0 ? 0 : length > a.prompt_cap ? a.prompt_cap : length;
+  }
+  const Tokens path_tokens(said, before), prompt_tokens(a.d_prompt + p * a.prompt_stride, length);
+
+  const float* const bias = a.d_bias ? a.d_bias + p * a.bias_stride + from : nullptr;
+  const int64_t first_row = (int64_t)path * a.n;
+  const E* const in = static_cast<const E*>(a.d_logits) + first_row * a.logit_stride + from;
+  E* const out = static_cast<E*>(a.d_out) + first_row * a.out_stride + from;
+  // bit i: logit at + i of row t may be picked (at: a multiple of eight, from the stretch's first)
+  const auto allowed = [&](int32_t t, int32_t at) -> uint32_t {
+    return a.d_mask ? reinterpret_cast<const uint8_t*>(a.d_mask + (first_row + t) * a.mask_stride)[(from + at) / 8] : 0xff;
+  };
+  typedef E Eight __attribute__((ext_vector_type(8), aligned(sizeof(E))));
+  typedef float EightFloats __attribute__((ext_vector_type(8), aligned(4)));
+  typedef uint32_t EightWords __attribute__((ext_vector_type(8)));
+  constexpr int kAhead = 2;
+  const int32_t eights = size / 8, all = count * eights;
+  Eight x[kAhead];
+  uint32_t bits[kAhead];
+  int32_t t[kAhead], at[kAhead];
+  const auto ask = [&](int32_t x0) {
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+      const int32_t item = x0 + s * kThreads < all ? x0 + s * kThreads : x0;
+      t[s] = item / eights;
+      at[s] = 8 * (item - t[s] * eights);
+      x[s] = *reinterpret_cast<const Eight*>(in + t[s] * a.logit_stride + at[s]);
+      bits[s] = allowed(t[s], at[s]);
+    }
+  };
+  if ((int32_t)threadIdx.x < all) ask(threadIdx.x);
+
   if (penalties) {
     repetition = a.d_penalties[3 * (int64_t)p];
     presence = a.d_penalties[3 * (int64_t)p + 1];
     frequency = a.d_penalties[3 * (int64_t)p + 2];
-    for (int32_t x = threadIdx.x; x < per; x += kThreads) words[x] = 0;
-    if (a.d_tokens) {
-      path_len = a.d_path_len[path];
-      path_len = path_len < 0 ? 0 : path_len > a.path_cap ? a.path_cap : path_len;
-      before = path_len - count;
-    }
-    const int32_t* const said = a.d_tokens ? a.d_tokens + path * a.token_stride : nullptr;
+    for (int32_t x = threadIdx.x; x < per / 4; x += kThreads) reinterpret_cast<uint4*>(words)[x] = uint4{};
     if (threadIdx.x < CSD_MAX_VERIFY_STEP) {
       const int32_t at = before + (int32_t)threadIdx.x;
       newest[threadIdx.x] = said && (int32_t)threadIdx.x < count && at >= 0 ? said[at] : -1;
     }
     __syncthreads();
-    if (count) {
-      for (int32_t x = threadIdx.x; x < before; x += kThreads) {
-        const uint32_t v = (uint32_t)said[x] - (uint32_t)from;
-        if (v < (uint32_t)size) atomicAdd(&words[v], 1u);
-      }
-      if (a.d_prompt) {
-        int32_t length = a.d_prompt_len ? a.d_prompt_len[p] : a.prompt_cap;
-        length = length < 0 ? 0 : length > a.prompt_cap ? a.prompt_cap : length;
-        const int32_t* const prompt = a.d_prompt + p * a.prompt_stride;
-        for (int32_t x = threadIdx.x; x < length; x += kThreads) {
-          const uint32_t v = (uint32_t)prompt[x] - (uint32_t)from;
-          if (v < (uint32_t)size) atomicOr(&words[v], kPrompt);
-        }
-      }
-      if ((int32_t)threadIdx.x < count) {
-        const uint32_t v = (uint32_t)newest[threadIdx.x] - (uint32_t)from;
-        if (v < (uint32_t)size) atomicOr(&words[v], kNew);
-      }
+    path_tokens.each([&](uint32_t token) {
+      const uint32_t v = token - (uint32_t)from;
+      if (v < (uint32_t)size) atomicAdd(&words[v], 1u);
+    });
+    prompt_tokens.each([&](uint32_t token) {
+      const uint32_t v = token - (uint32_t)from;
+      if (v < (uint32_t)size) atomicOr(&words[v], kPrompt);
+    });
+    if ((int32_t)threadIdx.x < count) {
+      const uint32_t v = (uint32_t)newest[threadIdx.x] - (uint32_t)from;
+      if (v < (uint32_t)size) atomicOr(&words[v], kNew);
     }
     __syncthreads();
   }
-  for (int32_t t = 0; t < a.n; ++t) {
-    const int64_t row = (int64_t)path * a.n + t;
-    const E* const x = static_cast<const E*>(a.d_logits) + row * a.logit_stride + from;
-    E* const out = static_cast<E*>(a.d_out) + row * a.out_stride + from;
-    const float* const bias = a.d_bias ? a.d_bias + p * a.bias_stride + from : nullptr;
-    const uint32_t* const mask = a.d_mask ? a.d_mask + row * a.mask_stride : nullptr;
-    for (int32_t v = threadIdx.x; v < size; v += kThreads) {
-      float y = 0;
-      if (t < count) {
-        y = (float)x[v];
-        if (penalties) {
-          const uint32_t word = words[v];
-          if (word) {
-            int32_t times = word & (kNew - 1);
-            if (word & kNew)
-              for (int32_t i = 0; i <= t; ++i) times += newest[i] == from + v;
-            if (times || (word & kPrompt)) y = y > 0 ? y / repetition : y * repetition;
-            if (times) y -= frequency * (float)times + presence;
-          }
-        }
-        if (bias) y += bias[v];
-        if (mask && !(mask[(from + v) / 32] >> ((from + v) % 32) & 1)) y = -INFINITY;
+  const auto adjusted = [&](float y, uint32_t word, int32_t t, int32_t v) {
+    int32_t times = word & (kNew - 1);
+    if (word & kNew)
+      for (int32_t i = 0; i <= t; ++i) times += newest[i] == v;
+    if (times || (word & kPrompt)) y = y > 0 ? y / repetition : y * repetition;
+    if (times) y -= frequency * (float)times + presence;
+    return y;
+  };
+  for (int32_t x0 = threadIdx.x; x0 < all; x0 += kAhead * kThreads) {
+    if (x0 != (int32_t)threadIdx.x) ask(x0);
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+      if (x0 + s * kThreads >= all) break;
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = (float)x[s][i];
+      if (penalties) {
+        const EightWords word = *reinterpret_cast<const EightWords*>(words + at[s]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (word[i]) y[i] = adjusted(y[i], word[i], t[s], from + at[s] + i);
       }
-      out[v] = (E)y;
+      if (bias) {
+        const EightFloats b = *reinterpret_cast<const EightFloats*>(bias + at[s]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] += b[i];
+      }
+      Eight z;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] = (E)(bits[s] >> i & 1 ? y[i] : -INFINITY);
+      *reinterpret_cast<Eight*>(out + t[s] * a.out_stride + at[s]) = z;
     }
+  }
+  // the vocabulary's last few, and the rows of positions that there are none of
+  const int32_t rest = size % 8;
+  if ((int32_t)threadIdx.x < count * rest) {
+    const int32_t t = threadIdx.x / rest, i = threadIdx.x - t * rest, at = eights * 8 + i;
+    float y = (float)in[t * a.logit_stride + at];
+    if (penalties && words[at]) y = adjusted(y, words[at], t, from + at);
+    if (bias) y += bias[at];
+    out[t * a.out_stride + at] = (E)(allowed(t, eights * 8) >> i & 1 ? y : -INFINITY);
+  }
+  for (int32_t t = count; t < a.n; ++t) {
+    for (int32_t x = threadIdx.x; x < eights; x += kThreads) *reinterpret_cast<Eight*>(out + t * a.out_stride + 8 * x) = Eight{};
+    if ((int32_t)threadIdx.x < rest) out[t * a.out_stride + eights * 8 + threadIdx.x] = (E)0.0f;
   }
 }
 
-constexpr int32_t kMostLogits = 8192, kLeastLogits = 1024;
+constexpr int32_t kLeastLogits = 1024;
 
 }  // namespace
 }  // namespace verify
@@ -114,9 +198,10 @@ extern "C" int csd_adjust(const csd_adjustment* adjustment, void* stream) {
   if (a.d_tokens && (!a.d_path_len || a.token_stride < 0 || a.path_cap < 0 || a.path_cap > CSD_MAX_CACHE_TOKENS)) return CSD_ERR_INVALID_ARG;
   if (a.d_prompt && (a.prompt_stride < 0 || a.prompt_cap < 0 || a.prompt_cap > CSD_MAX_CACHE_TOKENS)) return CSD_ERR_INVALID_ARG;
   if ((a.d_bias && a.bias_stride < 0) || (a.d_mask && a.mask_stride < 0)) return CSD_ERR_INVALID_ARG;
-  // stretches: as long as leaves some 1024 workgroups
+  // stretches: as long as leaves some 1024 workgroups, up to 2048 .. 8192 logits
+  const int32_t longest = a.n <= 4 ? 8192 : a.n <= 8 ? 4096 : 2048;
   int64_t parts = (1024 + paths - 1) / paths;
-  const int64_t most = (a.vocab + kLeastLogits - 1) / kLeastLogits, least = (a.vocab + kMostLogits - 1) / kMostLogits;
+  const int64_t most = (a.vocab + kLeastLogits - 1) / kLeastLogits, least = (a.vocab + longest - 1) / longest;
   parts = parts < least ? least : parts > most ? most : parts;
   const int32_t per = (int32_t)(((a.vocab + parts - 1) / parts + 31) / 32 * 32);
   parts = (a.vocab + per - 1) / per;
@@ -125,7 +210,7 @@ extern "C" int csd_adjust(const csd_adjustment* adjustment, void* stream) {
   const int64_t together = ((int64_t)1 << 22) / parts;                // paths of a launch of less than 2^32 threads
   for (int64_t first = 0; first < paths; first += together) {
     const int64_t here = paths - first < together ? paths - first : together;
-    kernel<<<(uint32_t)(here * parts), 512, lds, static_cast<hipStream_t>(stream)>>>(a, (int32_t)first, (int32_t)parts, per);
+    kernel<<<(uint32_t)(here * parts), kThreads, lds, static_cast<hipStream_t>(stream)>>>(a, (int32_t)first, (int32_t)parts, per);
   }
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CSD_OK : csd::hip_fail(e, "csd_adjust");

@@ -2,7 +2,6 @@
 #include <cmath>
 
 #include "csd_cache.cuh"
-#include "csd_launch.h"
 #include "csd_rotate.cuh"
 
 namespace csd {
