@@ -15,14 +15,141 @@ struct PromptArgs {
   float* lse;
 };
 
-constexpr int kPromptRows = 128, kPromptBlocks = 2, kPromptTile = kBlock * kPromptBlocks;
+constexpr int kPromptRows = 128, kPromptTile = 2 * kBlock;
+
+// A wave's 32 query rows, as in Wave (csd_attend.cuh), from tiles of two blocks.
+template <class T, int D>
+struct PromptWave {
+  typedef typename T::One One;
+  typedef typename T::Eight Eight;
+  typedef Rows<D, false> R;
+  typedef Wave<T, D, false> W;
+  static constexpr int kTiles = D / 32, kStage = 4 * R::kHalf;            // keys of the tile's blocks, then values
+
+  W w;
+  uint32_t keys[D / 16], values[2][kTiles];              // where the lane reads in a block
+
+  __device__ void begin(float scale_log2, uint32_t ring) {
+    w.begin(scale_log2);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+      keys[c] = ring + (R::kSwizzled ? w.own_keys ^ c << 5 : w.own_keys + 32 * c);
+      asm("" : "+v"(keys[c]));                           // (kept, not worked out again)
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x) {
+        values[r][x] = ring + 2 * R::kHalf + (R::kSwizzled ? w.own_values[r] ^ x << 6 : w.own_values[r] + (x << 6));
+        asm("" : "+v"(values[r][x]));
+      }
+  }
+
+  __device__ void read_keys(Eight (&k)[D / 16], uint32_t at) const {
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) k[c] = lds_read<Eight>(keys[c] + at);
+  }
+  __device__ Acc scores(const Eight (&k)[D / 16]) const {
+    Acc s = T::mfma(k[0], w.q[0], Acc{});
+#pragma unroll
+    for (int c = 1; c < D / 16; ++c) s = T::mfma(k[c], w.q[c], s);
+    return s;
+  }
+  __device__ void read_values(Eight (&v)[kTiles][2], uint32_t at) const {
+    typedef short __attribute__((ext_vector_type(4))) Four;
+    typedef __attribute__((address_space(3))) Four* Place;
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const Pair lo = __builtin_bit_cast(Pair, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(uintptr_t)(values[0][x] + at + u * 16 * R::kRow)));
+        const Pair hi = __builtin_bit_cast(Pair, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(uintptr_t)(values[1][x] + at + u * 16 * R::kRow)));
+        v[x][u] = __builtin_bit_cast(Eight, Words{lo[0], lo[1], hi[0], hi[1]});
+      }
+  }
+  // A tile that all rows see whole, `at` in the ring.
+  __device__ void whole(uint32_t at) {
+    Eight k[D / 16];
+    read_keys(k, at);
+    __builtin_amdgcn_sched_barrier(0);
+    Acc s[2];
+    s[0] = T::mfma(k[0], w.q[0], Acc{});
+    k[0] = lds_read<Eight>(keys[0] + at + R::kHalf);
+#pragma unroll
+    for (int c = 1; c < D / 16; ++c) {
+      s[0] = T::mfma(k[c], w.q[c], s[0]);
+      k[c] = lds_read<Eight>(keys[c] + at + R::kHalf);
+      __builtin_amdgcn_sched_group_barrier(8, 1, 0);     // a product, a read
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    s[1] = scores(k);
+    Eight v[kTiles][2];
+    read_values(v, at);
+    __builtin_amdgcn_sched_barrier(0);
+    const uint32_t none[2] = {0, 0};
+    const int32_t seen[2] = {0, 0};
+    w.template softmax<false, 2>(s, none, seen);
+    Eight p[2][2];
+    W::weights(s[0], p[0]);
+    W::weights(s[1], p[1]);
+    __builtin_amdgcn_sched_barrier(0);
+    Eight u[kTiles][2];
+    read_values(u, at + R::kHalf);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w.o[x] = T::mfma(v[x][i], p[0][i], w.o[x]);
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w.o[x] = T::mfma(u[x][i], p[1][i], w.o[x]);
+  }
+
+  // A tile from token `from` on of which the lane's row sees those before `sees`, all of the wave's rows those before `all`, any those before `most`.
+  __device__ void edge(uint32_t ring, uint32_t at, int32_t from, int32_t sees, int32_t all, int32_t most) {
+    Acc s[2];
+    const uint32_t none[2] = {0, 0};
+    const int32_t seen[2] = {sees - from, sees - from - kBlock};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      Eight k[D / 16];
+      read_keys(k, at + e * R::kHalf);
+      s[e] = scores(k);
+    }
+    w.template softmax<true, 2>(s, none, seen);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int32_t base = from + e * kBlock;
+      const uint32_t block = ring + at + (2 + e) * R::kHalf;
+      if (__ballot(w.template values<true>(s[e], block, all - base, most - base)) == 0) continue;
+      // what values() has left out: infinities and NaN of tokens that some rows do not see
+      for (int32_t x = all - base < 0 ? 0 : all - base; x < kBlock && x < most - base; ++x) {
+        float own = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) own = token_of(r, w.half) == x ? s[e][r] : own;
+        const float other = __shfl_xor(own, 32);
+        const float weight = (float)(One)((x / 8 & 1) == w.half ? own : other);
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int d = 32 * i + (r & 3) + 8 * (r >> 2) + 4 * w.half;
+            const float v = (float)lds_read<One>(block + x * R::kRow + (((d / 8) ^ R::swizzle(x)) << 4) + d % 8 * 2);
+            if (base + x < sees && !(fabsf(v) < INFINITY)) w.o[i][r] += weight * v;
+          }
+      }
+    }
+  }
+};
 
 template <class T, int D>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_kernel(PromptArgs a) {
   typedef typename T::One One;
   typedef typename T::Eight Eight;
   typedef Rows<D, false> R;
-  constexpr int kStages = 2, kStage = 2 * kPromptBlocks * R::kHalf;      // keys of the tile's blocks, then values
+  constexpr int kStages = 2, kStage = PromptWave<T, D>::kStage;
   __shared__ alignas(512) uint8_t ring[kStages * kStage];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t head = blockIdx.x % (uint32_t)a.Hk;
@@ -31,8 +158,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_kernel(PromptArg
   if (first >= rows) return;
   const int32_t here = rows - first < kPromptRows ? (int32_t)(rows - first) : kPromptRows;
 
-  Wave<T, D, false> w;
-  w.begin(a.scale);
+  const uint32_t lds = uniform(lds_offset(ring));
+  PromptWave<T, D> p;
+  auto& w = p.w;
+  p.begin(a.scale, lds);
   const int32_t own = 32 * wave + (lane & 31);
   const bool valid = own < here;
   const int32_t token = (int32_t)((first + (valid ? own : 0)) / a.G), g = (int32_t)(first + (valid ? own : 0) - (int64_t)token * a.G);
@@ -57,71 +186,65 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_kernel(PromptArg
 
   const One* const keys = static_cast<const One*>(a.k.data) + seq.from * a.k.token_stride + head * a.k.head_stride;
   const One* const values = static_cast<const One*>(a.v.data) + seq.from * a.v.token_stride + head * a.v.head_stride;
-  const uint32_t lds = uniform(lds_offset(ring));
   // A piece of 1 KB has 64 chunks of 16 bytes; its lane i takes the one that lies at its place, of the sequence's last token where there
-  // is none.
-  constexpr int kPieces = R::kPieces * kPromptBlocks;    // of a tile's keys
-  auto load = [&](int32_t tile, int32_t stage) {
+  // is none.  Piece wave + 4 x of the tile's keys, of its values is the wave's.
+  constexpr int kPieces = 2 * R::kPieces / 4, kApart = 256 / R::kChunks;  // kApart: tokens from a piece of the wave's to its next
+  const auto place = [&](int x, uint32_t* token_in, uint32_t* within) {
+    const int chunk = (4 * x + wave) * 64 + lane;
+    *token_in = chunk / R::kChunks;
+    *within = (uint32_t)(chunk % R::kChunks ^ R::swizzle(*token_in & 31)) * 16;
+  };
+  uint32_t k_first, v_first;                             // where the lane reads for its first piece
+  {
+    uint32_t token_in, within;
+    place(0, &token_in, &within);
+    k_first = token_in * (uint32_t)a.k.token_stride * 2 + within;
+    v_first = token_in * (uint32_t)a.v.token_stride * 2 + within;
+  }
+  auto load = [&](int32_t tile, uint32_t to) {
+    const One* const k = keys + (int64_t)tile * kPromptTile * a.k.token_stride;
+    const One* const v = values + (int64_t)tile * kPromptTile * a.v.token_stride;
+    const int32_t left = seq.length - tile * kPromptTile;
+    const bool full = left >= kPromptTile;
 #pragma unroll
-    for (int x = 0; x < kPieces / 4; ++x) {
-      const int p = x * 4 + wave, chunk = p * 64 + lane, r = chunk / R::kChunks, c = chunk % R::kChunks;
-      int32_t t = tile * kPromptTile + r;
-      t = t < seq.length ? t : seq.length - 1;
-      const uint32_t within = (uint32_t)(c ^ R::swizzle(r & 31)) * 16;
-      const One* const k = keys + (int64_t)tile * kPromptTile * a.k.token_stride;
-      const One* const v = values + (int64_t)tile * kPromptTile * a.v.token_stride;
-      const uint32_t token_in = (uint32_t)(t - tile * kPromptTile);
-      fetch<R, 1>(uniform(lds + stage * kStage + 1024u * p), uniform(reinterpret_cast<const uint8_t*>(k)), 0, token_in * (uint32_t)a.k.token_stride * 2 + within);
-      fetch<R, 1>(uniform(lds + stage * kStage + kPromptBlocks * R::kHalf + 1024u * p), uniform(reinterpret_cast<const uint8_t*>(v)), 0, token_in * (uint32_t)a.v.token_stride * 2 + within);
+    for (int x = 0; x < kPieces; ++x) {
+      const uint32_t piece = to + 1024u * (4 * x + wave);
+      if (R::kSwizzled && full) {
+        const uint32_t turn = R::swizzle(x * kApart & 31) << 4;
+        fetch<R, 1>(uniform(lds + piece), uniform(reinterpret_cast<const uint8_t*>(k + x * kApart * a.k.token_stride)), 0, k_first ^ turn);
+        fetch<R, 1>(uniform(lds + piece + 2 * R::kHalf), uniform(reinterpret_cast<const uint8_t*>(v + x * kApart * a.v.token_stride)), 0, v_first ^ turn);
+      } else {
+        uint32_t token_in, within;
+        place(x, &token_in, &within);
+        token_in = (int32_t)token_in < left ? token_in : left - 1;
+        fetch<R, 1>(uniform(lds + piece), uniform(reinterpret_cast<const uint8_t*>(k)), 0, token_in * (uint32_t)a.k.token_stride * 2 + within);
+        fetch<R, 1>(uniform(lds + piece + 2 * R::kHalf), uniform(reinterpret_cast<const uint8_t*>(v)), 0, token_in * (uint32_t)a.v.token_stride * 2 + within);
+      }
     }
   };
   __builtin_amdgcn_s_waitcnt(0x0f70);                    // vmcnt(0): the queries are there
   load(0, 0);
-  for (int32_t j = 0; j < tiles; ++j) {
-    const int stage = j & 1;
+  const auto next = [&](int32_t j, uint32_t at) {
     wait_loads<0>();
-    meet();
-    if (j + 1 < tiles) load(j + 1, stage ^ 1);
-    const int32_t from = j * kPromptTile;
-    if (from >= most) continue;
-    const uint32_t b = lds + stage * kStage;
-    const uint32_t none[2] = {0, 0};
-    Acc s[2];
-    s[0] = w.scores(b, 0);
-    s[1] = w.scores(b + R::kHalf, 0);
-    const uint32_t vb = b + kPromptBlocks * R::kHalf;
-    if (from + kPromptTile <= all) {
-      const int32_t seen[2] = {};
-      w.template softmax<false, 2>(s, none, seen);
-      w.template values<false>(s[0], vb, 0, 0);
-      w.template values<false>(s[1], vb + R::kHalf, 0, 0);
-    } else {
-      const int32_t seen[2] = {sees - from, sees - from - kBlock};
-      w.template softmax<true, 2>(s, none, seen);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int32_t base = from + e * kBlock;
-        bool met = w.template values<true>(s[e], vb + e * R::kHalf, all - base, most - base);
-        if (__ballot(met) == 0) continue;
-        // what values() has left out: infinities and NaN of tokens that some rows do not see
-        const uint8_t* const block = ring + stage * kStage + (kPromptBlocks + e) * R::kHalf;
-        for (int32_t x = all - base < 0 ? 0 : all - base; x < kBlock && x < most - base; ++x) {
-          float own = 0;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) own = token_of(r, w.half) == x ? s[e][r] : own;
-          const float other = __shfl_xor(own, 32);
-          const float weight = (float)(One)((x / 8 & 1) == w.half ? own : other);
-#pragma unroll
-          for (int i = 0; i < Wave<T, D, false>::kTiles; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int d = 32 * i + (r & 3) + 8 * (r >> 2) + 4 * w.half;
-              const float v = (float)*reinterpret_cast<const One*>(block + x * R::kRow + (((d / 8) ^ R::swizzle(x)) << 4) + d % 8 * 2);
-              if (base + x < sees && !(fabsf(v) < INFINITY)) w.o[i][r] += weight * v;
-            }
-        }
-      }
-    }
+    meet();                                              // the tile is there, and all are done with the one before
+    if (j + 1 < tiles) load(j + 1, at ^ kStage);
+  };
+  const int32_t whole = all / kPromptTile < tiles ? all / kPromptTile : tiles;
+  int32_t j = 0;
+  for (; j + 2 <= whole; j += 2) {
+    next(j, 0);
+    p.whole(0);
+    next(j + 1, kStage);
+    p.whole(kStage);
+  }
+  if (j < whole) {
+    next(j++, 0);
+    p.whole(0);
+  }
+  for (; j < tiles; ++j) {
+    const uint32_t at = j % 2 * kStage;
+    next(j, at);
+    if (j * kPromptTile < most) p.edge(lds, at, j * kPromptTile, sees, all, most);
   }
 
   const float sum = both_sum(w.l), over = sum == 0.0f ? 0.0f : 1.0f / sum;
