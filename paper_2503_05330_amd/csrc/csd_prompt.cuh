@@ -107,8 +107,8 @@ struct PromptWave {
       for (int i = 0; i < 2; ++i) w.o[x] = T::mfma(u[x][i], p[1][i], w.o[x]);
   }
 
-  // A tile from token `from` on of which the lane's row sees those before `sees`, all of the wave's rows those before `all`, any those before `most`.
-  __device__ void edge(uint32_t ring, uint32_t at, int32_t from, int32_t sees, int32_t all, int32_t most) {
+  // A tile from token `from` on of which the lane's row sees those before `sees`, any of the wave's rows those before `most`.
+  __device__ void edge(uint32_t ring, uint32_t at, int32_t from, int32_t sees, int32_t most) {
     Acc s[2];
     const uint32_t none[2] = {0, 0};
     const int32_t seen[2] = {sees - from, sees - from - kBlock};
@@ -121,11 +121,30 @@ struct PromptWave {
     w.template softmax<true, 2>(s, none, seen);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
+      // Where the largest magnitude of the block's values is finite, weights of zero take care of what a row does not see.
+      typedef uint16_t __attribute__((ext_vector_type(2))) Halves;
+      Halves high{};
+      Eight v[kTiles][2];
+      read_values(v, at + e * R::kHalf);
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) high = __builtin_elementwise_max(high, __builtin_bit_cast(Halves, __builtin_bit_cast(Words, v[x][u])[i] & 0x7fff7fffu));
+      if (__ballot(high[0] >= T::kExponent || high[1] >= T::kExponent) == 0) {
+        Eight p[2];
+        W::weights(s[e], p);
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) w.o[x] = T::mfma(v[x][u], p[u], w.o[x]);
+        continue;
+      }
+      // Else 0 x infinity would reach rows that do not see the token: one token after the other, for the rows that do.
       const int32_t base = from + e * kBlock;
       const uint32_t block = ring + at + (2 + e) * R::kHalf;
-      if (__ballot(w.template values<true>(s[e], block, all - base, most - base)) == 0) continue;
-      // what values() has left out: infinities and NaN of tokens that some rows do not see
-      for (int32_t x = all - base < 0 ? 0 : all - base; x < kBlock && x < most - base; ++x) {
+      for (int32_t x = 0; x < kBlock && x < most - base; ++x) {
         float own = 0;
 #pragma unroll
         for (int r = 0; r < 16; ++r) own = token_of(r, w.half) == x ? s[e][r] : own;
@@ -137,7 +156,7 @@ struct PromptWave {
           for (int r = 0; r < 16; ++r) {
             const int d = 32 * i + (r & 3) + 8 * (r >> 2) + 4 * w.half;
             const float v = (float)lds_read<One>(block + x * R::kRow + (((d / 8) ^ R::swizzle(x)) << 4) + d % 8 * 2);
-            if (base + x < sees && !(fabsf(v) < INFINITY)) w.o[i][r] += weight * v;
+            if (base + x < sees) w.o[i][r] = fmaf(weight, v, w.o[i][r]);
           }
       }
     }
@@ -167,7 +186,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_kernel(PromptArg
   const int32_t token = (int32_t)((first + (valid ? own : 0)) / a.G), g = (int32_t)(first + (valid ? own : 0) - (int64_t)token * a.G);
   const int32_t sees = valid ? token + 1 : 0;
   const int64_t at = (int64_t)seq.from + token;
-  {
+  const auto queries = [&] {
     const One* const from = static_cast<const One*>(a.q.data) + at * a.q.token_stride + (int64_t)(head * a.G + g) * a.q.head_stride;
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
@@ -176,7 +195,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_kernel(PromptArg
       if (a.scale < 0) x ^= 0x80008000u;
       w.q[c] = __builtin_bit_cast(Eight, x);
     }
-  }
+  };
   // what all and what any of the wave's, of the workgroup's rows see
   const int32_t wave_here = here - 32 * wave;
   const int32_t all = wave_here > 0 ? (int32_t)((first + 32 * wave) / a.G) + 1 : 0;
@@ -222,8 +241,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_kernel(PromptArg
       }
     }
   };
-  __builtin_amdgcn_s_waitcnt(0x0f70);                    // vmcnt(0): the queries are there
   load(0, 0);
+  queries();
+  __builtin_amdgcn_s_waitcnt(0x0f70);                    // vmcnt(0), with the builtin, so that the compiler knows and does not wait for the queries in the loop
   const auto next = [&](int32_t j, uint32_t at) {
     wait_loads<0>();
     meet();                                              // the tile is there, and all are done with the one before
@@ -244,7 +264,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_kernel(PromptArg
   for (; j < tiles; ++j) {
     const uint32_t at = j % 2 * kStage;
     next(j, at);
-    if (j * kPromptTile < most) p.edge(lds, at, j * kPromptTile, sees, all, most);
+    if (j * kPromptTile < most) p.edge(lds, at, j * kPromptTile, sees, most);
   }
 
   const float sum = both_sum(w.l), over = sum == 0.0f ? 0.0f : 1.0f / sum;

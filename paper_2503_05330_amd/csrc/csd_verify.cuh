@@ -138,11 +138,12 @@ __device__ inline Sequence sequence_of(const int32_t* offsets, int32_t count, in
     return x < 0 ? 0 : x > tokens ? tokens : x;
   };
   const auto first = [&](int32_t from, int32_t s) { return (uint32_t)((uint64_t)from * per / wide) + (uint32_t)s; };
-  int32_t low = 0, high = count;     // the last sequence that begins at the tile or before it is in [low, high)
+  int32_t low = 0, high = count;     // the last sequence that begins at the tile or before it is in [low, high): 64 places looked at at once
   while (high - low > 1) {
-    const int32_t mid = (low + high) / 2;
-    if (first(offset(mid), mid) <= tile) low = mid;
-    else high = mid;
+    const int32_t apart = (high - low + 63) / 64, at = low + (int32_t)(threadIdx.x & 63) * apart;
+    const int32_t before = __popcll(__ballot(at < high && first(offset(at < high ? at : low), at) <= tile));
+    if (before > 1) low += (before - 1) * apart;
+    high = high - low < apart ? high : low + apart;
   }
   Sequence s;
   s.which = low;
