@@ -34,58 +34,60 @@ struct PromptWave {
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
       keys[c] = ring + (R::kSwizzled ? w.own_keys ^ c << 5 : w.own_keys + 32 * c);
-      asm("" : "+v"(keys[c]));                           // (kept, not worked out again)
+      if constexpr (D <= 128) asm("" : "+v"(keys[c]));   // (kept, not worked out again)
     }
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
       for (int x = 0; x < kTiles; ++x) {
         values[r][x] = ring + 2 * R::kHalf + (R::kSwizzled ? w.own_values[r] ^ x << 6 : w.own_values[r] + (x << 6));
-        asm("" : "+v"(values[r][x]));
+        if constexpr (D <= 128) asm("" : "+v"(values[r][x]));
       }
   }
 
-  __device__ void read_keys(Eight (&k)[D / 16], uint32_t at) const {
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) k[c] = lds_read<Eight>(keys[c] + at);
-  }
-  __device__ Acc scores(const Eight (&k)[D / 16]) const {
-    Acc s = T::mfma(k[0], w.q[0], Acc{});
-#pragma unroll
-    for (int c = 1; c < D / 16; ++c) s = T::mfma(k[c], w.q[c], s);
-    return s;
-  }
-  __device__ void read_values(Eight (&v)[kTiles][2], uint32_t at) const {
+  // eight d's of a token: the `c`th operand of block e's scores
+  __device__ Eight key(uint32_t at, int e, int c) const { return lds_read<Eight>(keys[c] + at + e * R::kHalf); }
+  struct Two {
+    Eight u[2];
+  };
+  // both operands of block e's values of d's 32 x ..
+  __device__ Two value(uint32_t at, int e, int x) const {
     typedef short __attribute__((ext_vector_type(4))) Four;
     typedef __attribute__((address_space(3))) Four* Place;
+    Two v;
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const Pair lo = __builtin_bit_cast(Pair, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(uintptr_t)(values[0][x] + at + u * 16 * R::kRow)));
-        const Pair hi = __builtin_bit_cast(Pair, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(uintptr_t)(values[1][x] + at + u * 16 * R::kRow)));
-        v[x][u] = __builtin_bit_cast(Eight, Words{lo[0], lo[1], hi[0], hi[1]});
-      }
-  }
-  // A tile that all rows see whole, `at` in the ring.
-  __device__ void whole(uint32_t at) {
-    Eight k[D / 16];
-    read_keys(k, at);
-    __builtin_amdgcn_sched_barrier(0);
-    Acc s[2];
-    s[0] = T::mfma(k[0], w.q[0], Acc{});
-    k[0] = lds_read<Eight>(keys[0] + at + R::kHalf);
-#pragma unroll
-    for (int c = 1; c < D / 16; ++c) {
-      s[0] = T::mfma(k[c], w.q[c], s[0]);
-      k[c] = lds_read<Eight>(keys[c] + at + R::kHalf);
-      __builtin_amdgcn_sched_group_barrier(8, 1, 0);     // a product, a read
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t to = at + e * R::kHalf + u * 16 * R::kRow;
+      const Pair lo = __builtin_bit_cast(Pair, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(uintptr_t)(values[0][x] + to)));
+      const Pair hi = __builtin_bit_cast(Pair, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(uintptr_t)(values[1][x] + to)));
+      v.u[u] = __builtin_bit_cast(Eight, Words{lo[0], lo[1], hi[0], hi[1]});
     }
+    return v;
+  }
+
+  // A tile that all rows see whole, `at` in the ring.  Operands are read kAhead products ahead, those of the values during the softmax: reads go
+  // on while products and exponentials do.
+  __device__ void whole(uint32_t at) {
+    constexpr int kKeys = 2 * (D / 16), kKeysAhead = 8;
+    Eight k[kKeysAhead];
+    Acc s[2];
+#pragma unroll
+    for (int i = 0; i < kKeysAhead; ++i) k[i] = key(at, i / (D / 16), i % (D / 16));
     __builtin_amdgcn_sched_barrier(0);
-    s[1] = scores(k);
-    Eight v[kTiles][2];
-    read_values(v, at);
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) {
+      const int e = i / (D / 16), c = i % (D / 16), next = i + kKeysAhead;
+      s[e] = T::mfma(k[i % kKeysAhead], w.q[c], c ? s[e] : Acc{});
+      if (next < kKeys) {
+        k[i % kKeysAhead] = key(at, next / (D / 16), next % (D / 16));
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                 // a product, a read
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+    }
+    constexpr int kValues = 2 * kTiles, kValuesAhead = 4;
+    Two v[kValuesAhead];
+#pragma unroll
+    for (int i = 0; i < kValuesAhead; ++i) v[i] = value(at, i / kTiles, i % kTiles);
     __builtin_amdgcn_sched_barrier(0);
     const uint32_t none[2] = {0, 0};
     const int32_t seen[2] = {0, 0};
@@ -94,71 +96,86 @@ struct PromptWave {
     W::weights(s[0], p[0]);
     W::weights(s[1], p[1]);
     __builtin_amdgcn_sched_barrier(0);
-    Eight u[kTiles][2];
-    read_values(u, at + R::kHalf);
-    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x)
+    for (int i = 0; i < kValues; ++i) {
+      const int e = i / kTiles, x = i % kTiles, next = i + kValuesAhead;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) w.o[x] = T::mfma(v[x][i], p[0][i], w.o[x]);
-#pragma unroll
-    for (int x = 0; x < kTiles; ++x)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) w.o[x] = T::mfma(u[x][i], p[1][i], w.o[x]);
+      for (int u = 0; u < 2; ++u) w.o[x] = T::mfma(v[i % kValuesAhead].u[u], p[e][u], w.o[x]);
+      if (next < kValues) {
+        v[i % kValuesAhead] = value(at, next / kTiles, next % kTiles);
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+      }
+    }
   }
 
-  // A tile from token `from` on of which the lane's row sees those before `sees`, any of the wave's rows those before `most`.
-  __device__ void edge(uint32_t ring, uint32_t at, int32_t from, int32_t sees, int32_t most) {
+  // A tile of which the lane's row sees the first `sees` tokens, any of the wave's rows the first `most`.
+  __device__ void edge(uint32_t ring, uint32_t at, int32_t sees, int32_t most) {
     Acc s[2];
-    const uint32_t none[2] = {0, 0};
-    const int32_t seen[2] = {sees - from, sees - from - kBlock};
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      Eight k[D / 16];
-      read_keys(k, at + e * R::kHalf);
-      s[e] = scores(k);
+      s[e] = Acc{};
+      if (e == 0 || most > kBlock) {
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) s[e] = T::mfma(key(at, e, c), w.q[c], s[e]);
+      }
     }
+    const uint32_t none[2] = {0, 0};
+    const int32_t seen[2] = {sees, sees - kBlock};
     w.template softmax<true, 2>(s, none, seen);
+    // Where the largest magnitude of a block's values is finite, weights of zero take care of what a row does not see.  Else 0 x infinity would
+    // reach rows that do not see the token: one token after the other, for the rows that do.
+    bool odd[2] = {false, false};
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      // Where the largest magnitude of the block's values is finite, weights of zero take care of what a row does not see.
+      if (e == 1 && most <= kBlock) break;
       typedef uint16_t __attribute__((ext_vector_type(2))) Halves;
       Halves high{};
-      Eight v[kTiles][2];
-      read_values(v, at + e * R::kHalf);
+      Two v[kTiles];
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x) v[x] = value(at, e, x);
 #pragma unroll
       for (int x = 0; x < kTiles; ++x)
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) high = __builtin_elementwise_max(high, __builtin_bit_cast(Halves, __builtin_bit_cast(Words, v[x][u])[i] & 0x7fff7fffu));
-      if (__ballot(high[0] >= T::kExponent || high[1] >= T::kExponent) == 0) {
-        Eight p[2];
-        W::weights(s[e], p);
+          for (int j = 0; j < 4; ++j) high = __builtin_elementwise_max(high, __builtin_bit_cast(Halves, __builtin_bit_cast(Words, v[x].u[u])[j] & 0x7fff7fffu));
+      odd[e] = __ballot(high[0] >= T::kExponent || high[1] >= T::kExponent) != 0;
+      if (odd[e]) continue;
+      Eight p[2];
+      W::weights(s[e], p);
 #pragma unroll
-        for (int x = 0; x < kTiles; ++x)
+      for (int x = 0; x < kTiles; ++x)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) w.o[x] = T::mfma(v[x][u], p[u], w.o[x]);
-        continue;
-      }
-      // Else 0 x infinity would reach rows that do not see the token: one token after the other, for the rows that do.
-      const int32_t base = from + e * kBlock;
-      const uint32_t block = ring + at + (2 + e) * R::kHalf;
-      for (int32_t x = 0; x < kBlock && x < most - base; ++x) {
-        float own = 0;
+        for (int u = 0; u < 2; ++u) w.o[x] = T::mfma(v[x].u[u], p[u], w.o[x]);
+    }
+    if (!odd[0] && !odd[1]) return;
+#pragma unroll 1
+    for (int e = 0; e < 2; ++e) {
+      if (!(e ? odd[1] : odd[0])) continue;
+      Acc t;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) own = token_of(r, w.half) == x ? s[e][r] : own;
-        const float other = __shfl_xor(own, 32);
-        const float weight = (float)(One)((x / 8 & 1) == w.half ? own : other);
+      for (int r = 0; r < 16; ++r) t[r] = e ? s[1][r] : s[0][r];
+      one_by_one(t, ring + at + (2 + e) * R::kHalf, sees - e * kBlock, most - e * kBlock);
+    }
+  }
+
+  // O of a block's tokens one after the other, each for the rows that see it; values: where they lie
+  __device__ void one_by_one(const Acc& s, uint32_t values, int32_t sees, int32_t most) {
+    for (int32_t x = 0; x < kBlock && x < most; ++x) {
+      float own = 0;
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i)
+      for (int r = 0; r < 16; ++r) own = token_of(r, w.half) == x ? s[r] : own;
+      const float other = __shfl_xor(own, 32);
+      const float weight = (float)(One)((x / 8 & 1) == w.half ? own : other);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int d = 32 * i + (r & 3) + 8 * (r >> 2) + 4 * w.half;
-            const float v = (float)lds_read<One>(block + x * R::kRow + (((d / 8) ^ R::swizzle(x)) << 4) + d % 8 * 2);
-            if (base + x < sees) w.o[i][r] = fmaf(weight, v, w.o[i][r]);
-          }
-      }
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int d = 32 * i + (r & 3) + 8 * (r >> 2) + 4 * w.half;
+          const float v = (float)lds_read<One>(values + x * R::kRow + (((d / 8) ^ R::swizzle(x)) << 4) + d % 8 * 2);
+          if (x < sees) w.o[i][r] = fmaf(weight, v, w.o[i][r]);
+        }
     }
   }
 };
@@ -264,23 +281,36 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_kernel(PromptArg
   for (; j < tiles; ++j) {
     const uint32_t at = j % 2 * kStage;
     next(j, at);
-    if (j * kPromptTile < most) p.edge(lds, at, j * kPromptTile, sees, most);
+    const int32_t from = j * kPromptTile;
+    if (most > from) p.edge(lds, at, sees - from, most - from);
   }
 
   const float sum = both_sum(w.l), over = sum == 0.0f ? 0.0f : 1.0f / sum;
-  if (!valid) return;
   const int64_t row = at * a.Hk * a.G + head * a.G + g;
-  if (a.lse && w.half == 0) a.lse[row] = sum == 0.0f ? kNone : (w.m + __builtin_amdgcn_logf(sum)) * 0.693147180559945309f;
+  if (valid && a.lse && w.half == 0) a.lse[row] = sum == 0.0f ? kNone : (w.m + __builtin_amdgcn_logf(sum)) * 0.693147180559945309f;
   One* const out = static_cast<One*>(a.out) + row * D;
+  // A lane has four d's of every eight of its row, that 32 away the others: one takes all of an eight, the other of the next.
 #pragma unroll
   for (int x = 0; x < D / 32; ++x)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      typedef One __attribute__((ext_vector_type(4))) Four;
-      Four y;
+    for (int j = 0; j < 4; j += 2) {
+      union {
+        One one[4];
+        uint32_t word[2];
+      } y, z;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) y[r] = (One)(w.o[x][4 * j + r] * over);
-      *reinterpret_cast<Four*>(out + 32 * x + 8 * j + 4 * w.half) = y;
+      for (int r = 0; r < 4; ++r) {
+        y.one[r] = (One)(w.o[x][4 * j + r] * over);
+        z.one[r] = (One)(w.o[x][4 * j + 4 + r] * over);
+      }
+      Words all;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const auto both = __builtin_amdgcn_permlane32_swap(y.word[i], z.word[i], false, false);
+        all[i] = both[0];
+        all[2 + i] = both[1];
+      }
+      if (valid) *reinterpret_cast<Words*>(out + 32 * x + 8 * j + 8 * w.half) = all;
     }
 }
 
