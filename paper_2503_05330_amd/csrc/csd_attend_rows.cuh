@@ -69,7 +69,7 @@ __device__ inline int32_t pack_tokens(const AttendArgs& a, int32_t p, int32_t fi
   return before;
 }
 
-// ---- loads to LDS.  The first wait is for the wave's own reads of the stage that is written.
+// ---- loads to LDS.
 
 // (the same for all lanes: in scalar registers, whatever the compiler can tell)
 __device__ inline uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
@@ -83,29 +83,41 @@ __device__ inline const uint8_t* uniform(const uint8_t* p) {
 // never keeps it for a program.)
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
+// Pieces of 1 KB that lie behind each other in LDS, 16 bytes of each from every lane: from + source, 1024 bytes less for every piece before.
+__device__ inline void fetch(uint32_t lds, const uint8_t* from, const uint32_t (&source)[4]) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
+      "global_load_lds_dwordx4 %2, %5 offset:1024\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048\n\t"
+      "global_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds), "v"(source[0]), "v"(source[1]), "v"(source[2]), "v"(source[3]), "s"(from) : "m0", "memory");
+}
+__device__ inline void fetch(uint32_t lds, const uint8_t* from, const uint32_t (&source)[2]) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds),
+               "v"(source[0]), "v"(source[1]), "s"(from) : "m0", "memory");
+}
+__device__ inline void fetch(uint32_t lds, const uint8_t* from, uint32_t source) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(source), "s"(from) : "m0", "memory");
+}
+// until the wave's own reads of LDS are done, so that what they read may be written
+__device__ inline void own_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 // N pieces of 1 KB from piece p on
 template <class R, int N>
 __device__ inline void fetch(uint32_t lds, const uint8_t* from, int p, uint32_t source) {
+  own_reads_done();
   if constexpr (N >= 4) {
-    asm volatile(
-        "s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
-        "global_load_lds_dwordx4 %2, %5 offset:1024\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-        "global_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds), "v"(source ^ R::turn(p)), "v"(source ^ R::turn(p + 1)),
-        "v"(source ^ R::turn(p + 2)), "v"(source ^ R::turn(p + 3)), "s"(from) : "m0", "memory");
+    fetch(lds, from, {source ^ R::turn(p), source ^ R::turn(p + 1), source ^ R::turn(p + 2), source ^ R::turn(p + 3)});
     if constexpr (N > 4) fetch<R, N - 4>(lds + 4096, from + 4096, p + 4, source);
   } else if constexpr (N >= 2) {
-    asm volatile(
-        "s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
-        "global_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds), "v"(source ^ R::turn(p)), "v"(source ^ R::turn(p + 1)), "s"(from) : "m0", "memory");
+    fetch(lds, from, {source ^ R::turn(p), source ^ R::turn(p + 1)});
     if constexpr (N > 2) fetch<R, N - 2>(lds + 2048, from + 2048, p + 2, source);
   } else {
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(source ^ R::turn(p)), "s"(from) : "m0", "memory");
+    fetch(lds, from, source ^ R::turn(p));
   }
 }
 // 64 bytes, 4 from each of the first sixteen lanes
 __device__ inline void fetch_scales(uint32_t lds, const uint8_t* from, int lane) {
+  own_reads_done();
   if (lane < 16)
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(lane * 4), "s"(from) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(lane * 4), "s"(from) : "m0", "memory");
 }
 #pragma clang diagnostic pop
 // until no more than N of the wave's loads are under way

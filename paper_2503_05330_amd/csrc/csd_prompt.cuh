@@ -15,7 +15,108 @@ struct PromptArgs {
   float* lse;
 };
 
-constexpr int kPromptRows = 128, kPromptTile = 2 * kBlock;
+constexpr int kPromptTile = 2 * kBlock, kPromptStages = 2;
+
+// The item of a workgroup: a tile of `wide` rows of a sequence, for a kv head.  Of up to 64 sequences the longest go first, each from its last tile
+// (the longest run of tokens) on, so that no long item is left for the end, while the items at work at a time share their tokens.
+// false: there is none.
+constexpr int32_t kSorted = 16, kSortedItems = 3072;
+__device__ inline bool sorted_item(const PromptArgs& a, uint32_t block, int32_t wide, bool pairs, Sequence* seq, int32_t* head) {
+  const int32_t lane = threadIdx.x & 63;
+  const auto offset = [&](int32_t i) {
+    const int32_t y = a.offsets[i < a.sequences ? i : a.sequences];
+    return y < 0 ? 0 : y > a.tokens ? a.tokens : y;
+  };
+  const int32_t from = offset(lane), end = offset(lane + 1), length = end > from ? end - from : 0;
+  const int32_t tiles = (int32_t)(((int64_t)length * a.G + wide - 1) / wide);
+  const int32_t key = tiles << 6 | (63 - lane);          // (tiles: below 2^23)
+  int32_t start = 0, all = 0;                            // the tiles before the sequence's, and in all
+  for (int32_t x0 = 0; x0 < a.sequences; x0 += 8)        // (lanes of no sequence have no tiles)
+#pragma unroll
+    for (int32_t x = 0; x < 8; ++x) {
+      const int32_t other = __builtin_amdgcn_readlane(key, x0 + x);
+      start += other > key ? other >> 6 : 0;
+      all += other >> 6;
+    }
+  const uint32_t items = (uint32_t)all * (uint32_t)a.Hk;
+  if (block >= items) return false;
+  // Where all are there at once, two a CU, a CU's second is one of the shortest if its first is one of the longest.
+  constexpr uint32_t kCUs = 256;
+  if (pairs && items <= 2 * kCUs && block >= kCUs) block = items - 1 - (block - kCUs);
+  const int32_t nth = (int32_t)(block / (uint32_t)a.Hk);
+  *head = (int32_t)(block - (uint32_t)nth * (uint32_t)a.Hk);
+  const int at = __ffsll((unsigned long long)__ballot(start <= nth && nth < start + tiles)) - 1;
+  seq->which = at;
+  seq->from = __builtin_amdgcn_readlane(from, at);
+  seq->length = __builtin_amdgcn_readlane(length, at);
+  seq->tile = __builtin_amdgcn_readlane(tiles, at) - 1 - (nth - __builtin_amdgcn_readlane(start, at));
+  return true;
+}
+
+// A wave's share of the loads of a tile's keys, or of its values: pieces of 1 KB, 64 chunks of 16 bytes each; lane i takes the one that lies at
+// its place, of the sequence's last token (`left`: its tokens from the tile's first on) where there is none.
+template <class R, int WAVES>
+struct TileLoads {
+  static constexpr int kPieces = 2 * R::kPieces / WAVES, kApart = 64 * WAVES / R::kChunks;       // piece wave + WAVES x; tokens from one to the next
+  static constexpr bool kAlike = R::kSwizzled;           // the lane's places in its pieces differ by whole tokens and a constant order of chunks
+  uint32_t at[kAlike ? 1 : kPieces];
+  static __device__ uint32_t place(int x, int64_t stride, int32_t left, int wave, int lane) {
+    const int chunk = (wave + WAVES * x) * 64 + lane, row = chunk / R::kChunks, token = row < left ? row : left - 1;
+    return (uint32_t)token * (uint32_t)stride * 2 + (uint32_t)(chunk % R::kChunks ^ R::swizzle(row & 31)) * 16;
+  }
+  __device__ TileLoads(int64_t stride, int wave, int lane) {
+#pragma unroll
+    for (int x = 0; x < (kAlike ? 1 : kPieces); ++x) at[x] = place(x, stride, kPromptTile, wave, lane);
+  }
+  // a tile whose tokens are all there
+  template <class One>
+  __device__ void fetch_to(uint32_t lds, const One* from, int64_t stride, int wave) const {
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      const uint32_t to = uniform(lds + 1024u * (WAVES * x + wave));
+      if constexpr (kAlike) fetch(to, uniform(reinterpret_cast<const uint8_t*>(from + x * kApart * stride)), at[0] ^ R::swizzle(x * kApart & 31) << 4);
+      else fetch(to, uniform(reinterpret_cast<const uint8_t*>(from)), at[x]);
+    }
+  }
+  template <class One>
+  static __device__ void fetch_part(uint32_t lds, const One* from, int64_t stride, int32_t left, int wave, int lane) {
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x)
+      fetch(uniform(lds + 1024u * (WAVES * x + wave)), uniform(reinterpret_cast<const uint8_t*>(from)), place(x, stride, left, wave, lane));
+  }
+};
+
+// A lane's results: O / l of its row, half of the d's, and lse.
+template <class T, int D>
+__device__ inline void write_row(const PromptArgs& a, const Acc (&o)[D / 32], float m, float l, int64_t row, bool valid, int half) {
+  typedef typename T::One One;
+  const float sum = both_sum(l), over = sum == 0.0f ? 0.0f : 1.0f / sum;
+  if (valid && a.lse && half == 0) a.lse[row] = sum == 0.0f ? kNone : (m + __builtin_amdgcn_logf(sum)) * 0.693147180559945309f;
+  One* const out = static_cast<One*>(a.out) + row * D;
+  // A lane has four d's of every eight of its row, that 32 away the others: one takes all of an eight, the other of the next.
+#pragma unroll
+  for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+      union {
+        One one[4];
+        uint32_t word[2];
+      } y, z;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        y.one[r] = (One)(o[x][4 * j + r] * over);
+        z.one[r] = (One)(o[x][4 * j + 4 + r] * over);
+      }
+      Words all;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const auto both = __builtin_amdgcn_permlane32_swap(y.word[i], z.word[i], false, false);
+        all[i] = both[0];
+        all[2 + i] = both[1];
+      }
+      if (valid) *reinterpret_cast<Words*>(out + 32 * x + 8 * j + 8 * half) = all;
+    }
+}
 
 // A wave's 32 query rows, as in Wave (csd_attend.cuh), from tiles of two blocks.
 template <class T, int D>
@@ -180,16 +281,23 @@ struct PromptWave {
   }
 };
 
-template <class T, int D>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_kernel(PromptArgs a) {
+template <class T, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D <= 128 ? 2 : 1) void prompt_kernel(PromptArgs a) {
+  constexpr int kPromptRows = 32 * WAVES;
   typedef typename T::One One;
   typedef typename T::Eight Eight;
   typedef Rows<D, false> R;
-  constexpr int kStages = 2, kStage = PromptWave<T, D>::kStage;
-  __shared__ alignas(512) uint8_t ring[kStages * kStage];
+  constexpr int kStage = PromptWave<T, D>::kStage;
+  extern __shared__ __align__(512) uint8_t ring[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int32_t head = blockIdx.x % (uint32_t)a.Hk;
-  const Sequence seq = sequence_of(a.offsets, a.sequences, a.tokens, a.tiles - 1 - blockIdx.x / (uint32_t)a.Hk, kPromptRows, a.G);
+  int32_t head;
+  Sequence seq;
+  if (a.sequences <= kSorted && (int64_t)a.tiles * a.Hk <= kSortedItems) {
+    if (!sorted_item(a, blockIdx.x, kPromptRows, WAVES == 4 && D <= 128, &seq, &head)) return;
+  } else {
+    head = blockIdx.x % (uint32_t)a.Hk;
+    seq = sequence_of(a.offsets, a.sequences, a.tokens, a.tiles - 1 - blockIdx.x / (uint32_t)a.Hk, kPromptRows, a.G);
+  }
   const int64_t rows = (int64_t)seq.length * a.G, first = (int64_t)seq.tile * kPromptRows;
   if (first >= rows) return;
   const int32_t here = rows - first < kPromptRows ? (int32_t)(rows - first) : kPromptRows;
@@ -222,40 +330,19 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_kernel(PromptArg
 
   const One* const keys = static_cast<const One*>(a.k.data) + seq.from * a.k.token_stride + head * a.k.head_stride;
   const One* const values = static_cast<const One*>(a.v.data) + seq.from * a.v.token_stride + head * a.v.head_stride;
-  // A piece of 1 KB has 64 chunks of 16 bytes; its lane i takes the one that lies at its place, of the sequence's last token where there
-  // is none.  Piece wave + 4 x of the tile's keys, of its values is the wave's.
-  constexpr int kPieces = 2 * R::kPieces / 4, kApart = 256 / R::kChunks;  // kApart: tokens from a piece of the wave's to its next
-  const auto place = [&](int x, uint32_t* token_in, uint32_t* within) {
-    const int chunk = (4 * x + wave) * 64 + lane;
-    *token_in = chunk / R::kChunks;
-    *within = (uint32_t)(chunk % R::kChunks ^ R::swizzle(*token_in & 31)) * 16;
-  };
-  uint32_t k_first, v_first;                             // where the lane reads for its first piece
-  {
-    uint32_t token_in, within;
-    place(0, &token_in, &within);
-    k_first = token_in * (uint32_t)a.k.token_stride * 2 + within;
-    v_first = token_in * (uint32_t)a.v.token_stride * 2 + within;
-  }
-  auto load = [&](int32_t tile, uint32_t to) {
+  typedef TileLoads<R, WAVES> Loads;
+  const Loads of_keys(a.k.token_stride, wave, lane), of_values(a.v.token_stride, wave, lane);
+  // (the wave has read what lies in the stage: it waits for its reads before the barrier that all loads stand behind)
+  const auto load = [&](int32_t tile, uint32_t to) {
+    const int32_t left = seq.length - tile * kPromptTile;
     const One* const k = keys + (int64_t)tile * kPromptTile * a.k.token_stride;
     const One* const v = values + (int64_t)tile * kPromptTile * a.v.token_stride;
-    const int32_t left = seq.length - tile * kPromptTile;
-    const bool full = left >= kPromptTile;
-#pragma unroll
-    for (int x = 0; x < kPieces; ++x) {
-      const uint32_t piece = to + 1024u * (4 * x + wave);
-      if (R::kSwizzled && full) {
-        const uint32_t turn = R::swizzle(x * kApart & 31) << 4;
-        fetch<R, 1>(uniform(lds + piece), uniform(reinterpret_cast<const uint8_t*>(k + x * kApart * a.k.token_stride)), 0, k_first ^ turn);
-        fetch<R, 1>(uniform(lds + piece + 2 * R::kHalf), uniform(reinterpret_cast<const uint8_t*>(v + x * kApart * a.v.token_stride)), 0, v_first ^ turn);
-      } else {
-        uint32_t token_in, within;
-        place(x, &token_in, &within);
-        token_in = (int32_t)token_in < left ? token_in : left - 1;
-        fetch<R, 1>(uniform(lds + piece), uniform(reinterpret_cast<const uint8_t*>(k)), 0, token_in * (uint32_t)a.k.token_stride * 2 + within);
-        fetch<R, 1>(uniform(lds + piece + 2 * R::kHalf), uniform(reinterpret_cast<const uint8_t*>(v)), 0, token_in * (uint32_t)a.v.token_stride * 2 + within);
-      }
+    if (left >= kPromptTile) {
+      of_keys.fetch_to(lds + to, k, a.k.token_stride, wave);
+      of_values.fetch_to(lds + to + 2 * R::kHalf, v, a.v.token_stride, wave);
+    } else {
+      Loads::fetch_part(lds + to, k, a.k.token_stride, left, wave, lane);
+      Loads::fetch_part(lds + to + 2 * R::kHalf, v, a.v.token_stride, left, wave, lane);
     }
   };
   load(0, 0);
@@ -285,40 +372,25 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_kernel(PromptArg
     if (most > from) p.edge(lds, at, sees - from, most - from);
   }
 
-  const float sum = both_sum(w.l), over = sum == 0.0f ? 0.0f : 1.0f / sum;
-  const int64_t row = at * a.Hk * a.G + head * a.G + g;
-  if (valid && a.lse && w.half == 0) a.lse[row] = sum == 0.0f ? kNone : (w.m + __builtin_amdgcn_logf(sum)) * 0.693147180559945309f;
-  One* const out = static_cast<One*>(a.out) + row * D;
-  // A lane has four d's of every eight of its row, that 32 away the others: one takes all of an eight, the other of the next.
-#pragma unroll
-  for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-    for (int j = 0; j < 4; j += 2) {
-      union {
-        One one[4];
-        uint32_t word[2];
-      } y, z;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        y.one[r] = (One)(w.o[x][4 * j + r] * over);
-        z.one[r] = (One)(w.o[x][4 * j + 4 + r] * over);
-      }
-      Words all;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const auto both = __builtin_amdgcn_permlane32_swap(y.word[i], z.word[i], false, false);
-        all[i] = both[0];
-        all[2 + i] = both[1];
-      }
-      if (valid) *reinterpret_cast<Words*>(out + 32 * x + 8 * j + 8 * w.half) = all;
-    }
+  write_row<T, D>(a, w.o, w.m, w.l, at * a.Hk * a.G + head * a.G + g, valid, w.half);
 }
 
+template <class T, int D, int WAVES>
+void prompt_as(PromptArgs a, hipStream_t st) {
+  a.tiles = (int32_t)((int64_t)a.tokens * a.G / (32 * WAVES) + a.sequences);
+  prompt_kernel<T, D, WAVES><<<(uint32_t)a.tiles * (uint32_t)a.Hk, 64 * WAVES, kPromptStages * PromptWave<T, D>::kStage, st>>>(a);
+}
+template <class T, int D>
+void prompt_of(const PromptArgs& a, hipStream_t st) {
+  const int64_t rows = (int64_t)a.tokens * a.G;
+  if constexpr (D == 96 || D == 128) {
+    if (rows >= 4096 * (int64_t)a.sequences && rows / 256 * a.Hk >= 512) return prompt_as<T, D, 8>(a, st);
+  }
+  prompt_as<T, D, 4>(a, st);
+}
 template <int D>
 void prompt_of(const PromptArgs& a, bool f16, hipStream_t st) {
-  const uint32_t grid = (uint32_t)a.tiles * (uint32_t)a.Hk;
-  if (f16) prompt_kernel<F16, D><<<grid, 256, 0, st>>>(a);
-  else prompt_kernel<BF16, D><<<grid, 256, 0, st>>>(a);
+  f16 ? prompt_of<F16, D>(a, st) : prompt_of<BF16, D>(a, st);
 }
 
 void prompt_64(const PromptArgs& a, bool f16, hipStream_t st);

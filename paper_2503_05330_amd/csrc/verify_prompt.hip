@@ -18,7 +18,7 @@ extern "C" int csd_prompt_attend(const csd_heads* q, const csd_heads* k, const c
   if (!d_offsets || bad(d_offsets, 4) || (tokens && !d_out) || bad(d_out, 16) || bad(d_lse, 4)) return CSD_ERR_INVALID_ARG;
   if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 256) return CSD_ERR_UNIMPLEMENTED;
   const int32_t G = n_heads / n_kv_heads;
-  const int64_t tiles = tokens * G / kPromptRows + sequences;
+  const int64_t tiles = tokens * G / 128 + sequences;
   if (tiles * n_kv_heads > 1 << 23) return CSD_ERR_INVALID_ARG;
   if (tokens == 0) return CSD_OK;
   const PromptArgs a{*q, *k, *v, d_offsets, sequences, (int32_t)tokens, n_kv_heads, G, (int32_t)tiles, scale * 1.44269504088896340736f, d_out, d_lse};
