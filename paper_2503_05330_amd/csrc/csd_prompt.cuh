@@ -190,24 +190,46 @@ struct PromptWave {
 #pragma unroll
     for (int i = 0; i < kValuesAhead; ++i) v[i] = value(at, i / kTiles, i % kTiles);
     __builtin_amdgcn_sched_barrier(0);
-    const uint32_t none[2] = {0, 0};
-    const int32_t seen[2] = {0, 0};
-    w.template softmax<false, 2>(s, none, seen);
-    Eight p[2][2];
-    W::weights(s[0], p[0]);
-    W::weights(s[1], p[1]);
+    float most = s[0][0];                                // (as in Wave::softmax)
+#pragma unroll
+    for (int i = 1; i < 32; ++i) most = fmaxf(most, s[i / 16][i % 16]);
+    most = both_max(most) * w.scale;
+    if (__ballot(most > w.m + (W::kSlack + W::kLift))) {
+      const float high = fmaxf(w.m, most - W::kLift), down = w.m == kNone ? 0.0f : exp2_fast(w.m - high);
+      w.l *= down;
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x) w.o[x] *= down;
+      w.m = high;
+    }
     __builtin_amdgcn_sched_barrier(0);
+    const float base = w.m == kNone ? 0.0f : w.m;
+    Eight p[2][2];
+    const auto weights = [&](int e) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = exp2_fast(fmaf(s[e][r], w.scale, -base));
+        w.l += x;
+        p[e][r / 8][r % 8] = (One)x;
+      }
+    };
+    weights(0);
+    __builtin_amdgcn_sched_barrier(0);
+    // the second block's weights go between the products of the first's
+    weights(1);
 #pragma unroll
     for (int i = 0; i < kValues; ++i) {
       const int e = i / kTiles, x = i % kTiles, next = i + kValuesAhead;
 #pragma unroll
       for (int u = 0; u < 2; ++u) w.o[x] = T::mfma(v[i % kValuesAhead].u[u], p[e][u], w.o[x]);
-      if (next < kValues) {
-        v[i % kValuesAhead] = value(at, next / kTiles, next % kTiles);
-        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-      }
+      if (next < kValues) v[i % kValuesAhead] = value(at, next / kTiles, next % kTiles);
     }
+#pragma unroll
+    for (int i = 0; i < 2 * kTiles; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 56 / (2 * kTiles), 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
 
   // A tile of which the lane's row sees the first `sees` tokens, any of the wave's rows the first `most`.
