@@ -20,6 +20,8 @@
 #include <c10/core/GradMode.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 
+#include <cmath>
+
 #include "csd.h"
 #include "csd_verify.h"
 
@@ -471,7 +473,8 @@ PyObject* targets(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
 struct Device {
   void* stream;
   int64_t index;
-  explicit Device(Call& c) : stream(c.pointer()), index(c.integer()) {
+  explicit Device(Call& c) : Device(c, c.pointer()) {}
+  Device(Call& c, void* of) : stream(of), index(c.integer()) {
     if (index < 0 || index > 127) c.usual = false;
   }
   c10::Device device() const { return c10::Device(c10::DeviceType::CUDA, (c10::DeviceIndex)index); }
@@ -551,12 +554,12 @@ PyObject* rotate(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
-// cache_write_rotated(cache, stream, device, rotation, layer, q, k, v, positions, start, counts): (code, queries)
+// cache_write_rotated(cache, device, rotation, layer, q, k, v, positions, start, counts): (code, queries)
 PyObject* cache_write_rotated(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   Call c{args, n_args};
   const Cache x(c);
-  const Device d(c);
+  const Device d(c, x.stream);
   const Rotation r(c, d);
   const int32_t layer = c.small();
   int64_t n = 0;
@@ -598,7 +601,8 @@ PyObject* prompt_attend(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   const csd_heads v = packed_of(c, d, type, Hk, D, &n);
   const at::Tensor* o = peek(c, 1);
   const int32_t* offsets = ints_of(c, d, 2, false);
-  const float scale = c.real();
+  const bool usual_scale = c.at < c.n && c.args[c.at] == Py_None;
+  const float scale = usual_scale ? (float)(1 / std::sqrt((double)D)) : c.real();
   if (!c.usual || !o || o->dim() != 1 || o->numel() - 1 > INT32_MAX || H > INT32_MAX || Hk > INT32_MAX || D > INT32_MAX) Py_RETURN_NONE;
   const int64_t sizes[] = {n, H, D};
   Maker make(d.device());

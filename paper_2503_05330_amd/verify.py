@@ -233,7 +233,7 @@ class PathCache:
     def write_rotated(self, layer, q, k, v, rotary, positions, start=None, counts=None):
         """What rotate() does to q [P][N][n][heads][head_dim] and k at positions [P][N][n] int32, and write() with the rotated keys and v, in
         one launch.  Returns the rotated queries, all n of each path."""
-        got = _native.cache_write_rotated(*self._cache(), *_now(), *rotary._call, layer, q, k, v, positions, start, counts)
+        got = _native.cache_write_rotated(*self._cache(), torch._C._cuda_getDevice(), *rotary._call, layer, q, k, v, positions, start, counts)
         if got is not None:
             _check(got[0], "csd_cache_write_rotated")
             return got[1]
@@ -322,8 +322,11 @@ def _here(*tensors) -> None:
 
 
 def _now():
-    """The current stream and device."""
-    return _stream(), torch._C._cuda_getDevice()
+    """The current stream and device, of a tensor's calls in native code."""
+    if _native is None:
+        load()
+    device = torch._C._cuda_getDevice()
+    return torch._C._cuda_getCurrentRawStream(device), device
 
 
 def _packed(t: torch.Tensor, dtype, n_heads: int, dim: int) -> Heads:
@@ -353,8 +356,8 @@ def rotate(x: torch.Tensor, positions: torch.Tensor, rotary: Rotary, out: Option
     """Queries and keys x [..., heads, head_dim] (bfloat16, float16; a slice of a projection's output is fine) turned by their positions
     [...] int32: the first rotary.dim values of each head, the others as they are.  out: x itself, or another tensor of its shape."""
     if out is None and x.is_cuda:
-        load()
-        got = _native.rotate(*_now(), *rotary._call, x, positions)
+        now = _now()
+        got = _native.rotate(*now, *rotary._call, x, positions)
         if got is not None:
             _check(got[0], "csd_rotate")
             return got[1]
@@ -382,9 +385,9 @@ def prompt_attend(q, k, v, offsets, scale=None, out=None, lse=None):
     projection's output are fine), sequence s the tokens offsets[s] .. offsets[s + 1] - 1 (offsets int32, ascending), each of which sees
     those up to itself.  Returns [tokens][heads][head_dim]; lse: a float32 tensor [tokens][heads] that takes the logarithms of the sums.
     scale: 1 / sqrt(head_dim) where None.  Tokens of no sequence are not written (where out is None they hold anything)."""
-    if out is None and lse is None and q.is_cuda and q.dim() == 3:
-        load()
-        got = _native.prompt_attend(*_now(), q, k, v, offsets, q.shape[-1] ** -0.5 if scale is None else scale)
+    if out is None and lse is None and q.is_cuda:
+        now = _now()
+        got = _native.prompt_attend(*now, q, k, v, offsets, scale)
         if got is not None:
             _check(got[0], "csd_prompt_attend")
             return got[1]
@@ -417,8 +420,8 @@ def adjust(logits, tokens=None, path_len=None, counts=None, prompt=None, prompt_
     bias [P][vocab] or [vocab] float32 is added.  mask [P][N][n][words] or [words] int32: bit v % 32 of word v / 32 is 0
     where token v becomes -inf.  Positions beyond a path's count become zeros.  out: logits itself, or another tensor of its shape."""
     if logits.is_cuda:
-        load()
-        got = _native.adjust(*_now(), logits, tokens, path_len, counts, prompt, prompt_len, penalties, bias, mask, out)
+        now = _now()
+        got = _native.adjust(*now, logits, tokens, path_len, counts, prompt, prompt_len, penalties, bias, mask, out)
         if got is not None:
             _check(got[0], "csd_adjust")
             return got[1]
