@@ -166,25 +166,30 @@ struct PromptWave {
     return v;
   }
 
-  // A tile that all rows see whole, `at` in the ring.  Operands are read kAhead products ahead, those of the values during the softmax: reads go
-  // on while products and exponentials do.
-  __device__ void whole(uint32_t at) {
-    constexpr int kKeys = 2 * (D / 16), kKeysAhead = 8;
-    Eight k[kKeysAhead];
-    Acc s[2];
+  // The scores of a tile's first BLOCKS blocks, `at` in the ring: operands are read eight products ahead.
+  template <int BLOCKS>
+  __device__ void scores(Acc (&s)[2], uint32_t at) const {
+    constexpr int kKeys = BLOCKS * (D / 16), kAhead = kKeys < 8 ? kKeys : 8;
+    Eight k[kAhead];
 #pragma unroll
-    for (int i = 0; i < kKeysAhead; ++i) k[i] = key(at, i / (D / 16), i % (D / 16));
+    for (int i = 0; i < kAhead; ++i) k[i] = key(at, i / (D / 16), i % (D / 16));
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < kKeys; ++i) {
-      const int e = i / (D / 16), c = i % (D / 16), next = i + kKeysAhead;
-      s[e] = T::mfma(k[i % kKeysAhead], w.q[c], c ? s[e] : Acc{});
+      const int e = i / (D / 16), c = i % (D / 16), next = i + kAhead;
+      s[e] = T::mfma(k[i % kAhead], w.q[c], c ? s[e] : Acc{});
       if (next < kKeys) {
-        k[i % kKeysAhead] = key(at, next / (D / 16), next % (D / 16));
+        k[i % kAhead] = key(at, next / (D / 16), next % (D / 16));
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                 // a product, a read
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
     }
+  }
+
+  // A tile that all rows see whole, `at` in the ring.  Its values are read during the softmax.
+  __device__ void whole(uint32_t at) {
+    Acc s[2];
+    scores<2>(s, at);
     constexpr int kValues = 2 * kTiles, kValuesAhead = 4;
     Two v[kValuesAhead];
 #pragma unroll
@@ -235,13 +240,11 @@ struct PromptWave {
   // A tile of which the lane's row sees the first `sees` tokens, any of the wave's rows the first `most`.
   __device__ void edge(uint32_t ring, uint32_t at, int32_t sees, int32_t most) {
     Acc s[2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      s[e] = Acc{};
-      if (e == 0 || most > kBlock) {
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) s[e] = T::mfma(key(at, e, c), w.q[c], s[e]);
-      }
+    if (most > kBlock) {
+      scores<2>(s, at);
+    } else {
+      scores<1>(s, at);
+      s[1] = Acc{};
     }
     const uint32_t none[2] = {0, 0};
     const int32_t seen[2] = {sees, sees - kBlock};
