@@ -158,8 +158,8 @@ int csd_targets(const void* d_logits, int32_t type, int64_t rows, int32_t vocab,
                 void* stream);
 
 /* Rotary positions.  Pair i (of dim / 2) of a head at position t is turned by the angle 2 pi t turns[i]:
- *   (a, b) -> amplitude * (a cos - b sin, a sin + b cos), in 32 bits, rounded once.
- * Positions are whole numbers of any sign; turns and their product with a position are in 64 bits, so far positions lose nothing. */
+ *   (a, b) -> amplitude * (a cos - b sin, a sin + b cos), to 2^-35 of its terms, then rounded to 32 bits and to the type.
+ * Positions are whole numbers of any sign. */
 typedef struct {
   const double* d_turns; /* [dim / 2], device memory, 8-byte aligned: turns per token (csd_rotary_turns makes the usual ones)  */
   int32_t dim;           /* the first dim values of a head are rotated, the others copied: a multiple of 16, up to the head's   */

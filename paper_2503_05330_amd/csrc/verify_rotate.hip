@@ -24,18 +24,18 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
   typedef typename T::Eight Eight;
   typedef typename T::One Value;
-  extern __shared__ float2 turns[];                      // [token][pair]
+  extern __shared__ Turn turns[];
   const int64_t first = (int64_t)blockIdx.x * kGroup;
   const int32_t here = a.tokens - first < kGroup ? (int32_t)(a.tokens - first) : kGroup;
   const int32_t pairs = a.how.dim / 2;
   for (int32_t x = threadIdx.x; x < here * pairs; x += kThreads) {
     const int32_t token = x / pairs;
-    turns[x] = turn_of(a.how, a.positions[first + token], x - token * pairs);
+    Turns(turns, token, pairs)[x - token * pairs] = turn_of(a.how, a.positions[first + token], x - token * pairs);
   }
   __syncthreads();
   const int32_t head0 = blockIdx.y * a.per, heads = a.heads - head0 < a.per ? a.heads - head0 : a.per;
   const int32_t turning = a.how.dim / 16, units = turning + (a.dim - a.how.dim + 15) / 16, all = here * heads * units;
-  constexpr int kAhead = 4;
+  constexpr int kAhead = 2;                              // (4: 133 us for 131 with 8 x 4096 tokens of 40 heads of 128; a copy of as much takes 130)
   for (int32_t x0 = threadIdx.x; x0 < all; x0 += kAhead * kThreads) {
     Eight u[kAhead], v[kAhead];
     int64_t to[kAhead];
@@ -64,9 +64,18 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
       Value* const out = static_cast<Value*>(const_cast<void*>(a.out.data)) + to[s];
       Eight y = u[s], z = v[s];
       if (d[s] < a.how.dim) {
-        const float2* const own = turns + token[s] * pairs;
-        y = turned_eight<T>(u[s], v[s], d[s], a.how, own);
-        z = turned_eight<T>(v[s], u[s], e[s], a.how, own);
+        const Turns own(turns, token[s], pairs);
+        if (a.how.interleaved) {
+          y = turned_eight<T>(u[s], v[s], d[s], a.how, own);
+          z = turned_eight<T>(v[s], u[s], e[s], a.how, own);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {                  // a pair's turn, read once for both
+            const Turn t = own[d[s] + i];
+            y[i] = (Value)turned((float)u[s][i], (float)v[s][i], t);
+            z[i] = (Value)turned((float)v[s][i], -(float)u[s][i], t);
+          }
+        }
       }
       *reinterpret_cast<Eight*>(out + d[s]) = y;
       if (e[s] >= 0) *reinterpret_cast<Eight*>(out + e[s]) = z;
@@ -90,7 +99,7 @@ __global__ __launch_bounds__(kThreads) void place_kernel(PlaceArgs a) {
   typedef typename T::Eight Eight;
   typedef typename T::One Value;
   typedef Pieces<D> P;
-  __shared__ float2 turns[kGroup][D / 2];
+  __shared__ Turn turns[Turns::size(kGroup, D / 2)];
   const int wave = threadIdx.x >> 6, nth = (threadIdx.x & 63) / 8;
   const int64_t first = (int64_t)blockIdx.x * kGroup;
   const int32_t here = a.tokens - first < kGroup ? (int32_t)(a.tokens - first) : kGroup;
@@ -105,7 +114,7 @@ __global__ __launch_bounds__(kThreads) void place_kernel(PlaceArgs a) {
   const bool asked = there && t < count, live = asked && pos >= 0 && pos < m.held.cap;
   for (int32_t x = threadIdx.x; x < here * pairs; x += kThreads) {
     const int32_t of = x / pairs;
-    turns[of][x - of * pairs] = turn_of(a.how, a.positions[first + of], x - of * pairs);
+    Turns(turns, of, pairs)[x - of * pairs] = turn_of(a.how, a.positions[first + of], x - of * pairs);
   }
   if (wave == 0 && blockIdx.y == 0 && asked && !live) atomicOr(m.status, CSD_STATUS_CAPACITY);
   __syncthreads();
@@ -126,7 +135,7 @@ __global__ __launch_bounds__(kThreads) void place_kernel(PlaceArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < P::kPieces; ++i)
-      if (wanted && P::d(i) < a.how.dim) x[i] = turned_eight<T>(x[i], other[i], P::d(i), a.how, turns[nth]);
+      if (wanted && P::d(i) < a.how.dim) x[i] = turned_eight<T>(x[i], other[i], P::d(i), a.how, Turns(turns, nth, pairs));
   };
   const int32_t job0 = blockIdx.y * a.per, end = job0 + a.per < m.Hk + a.H ? job0 + a.per : m.Hk + a.H;
   for (int32_t job = job0 + wave; job < end; job += kMoveWaves) {
@@ -219,7 +228,7 @@ int csd_rotate(const csd_rotary* rotary, const csd_heads* x, const int32_t* d_po
   const RotateArgs a{*rotary, *x, *out, d_positions, tokens, heads, head_dim, per};
   const dim3 grid((uint32_t)groups, (uint32_t)((heads + per - 1) / per));
   auto* kernel = type == CSD_F16 ? rotate_kernel<F16> : rotate_kernel<BF16>;
-  kernel<<<grid, kThreads, kGroup * rotary->dim / 2 * sizeof(float2), static_cast<hipStream_t>(stream)>>>(a);
+  kernel<<<grid, kThreads, Turns::size(kGroup, rotary->dim / 2) * sizeof(Turn), static_cast<hipStream_t>(stream)>>>(a);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CSD_OK : csd::hip_fail(e, "csd_rotate");
 }
