@@ -174,7 +174,8 @@ int csd_rotary_turns(int32_t dim, double base, double factor, double original, d
 
 /* Rotates `tokens` tokens of `heads` heads of `head_dim` values (a multiple of 8, up to CSD_MAX_ROTATED_DIM).
  *   x, out       element d of head h of token t is data[t * token_stride + h * head_stride + d] (row_stride is not used); 16-byte aligned, strides
- *                multiples of 8.  out may be x itself, with the same strides; else they must not overlap.
+ *                multiples of 8.  out may be x itself, with the same strides; else they must not overlap,
+ *                nor out's heads each other.
  *   d_positions  [tokens] int32
  *   type         CSD_BF16 or CSD_F16 */
 int csd_rotate(const csd_rotary* rotary, const csd_heads* x, const int32_t* d_positions, int64_t tokens, int32_t heads, int32_t head_dim,

@@ -223,6 +223,11 @@ int csd_rotate(const csd_rotary* rotary, const csd_heads* x, const int32_t* d_po
   if (tokens && (!d_positions || misaligned(d_positions, 4))) return CSD_ERR_INVALID_ARG;
   if (x->data == out->data && ((tokens > 1 && x->token_stride != out->token_stride) || (heads > 1 && x->head_stride != out->head_stride))) return CSD_ERR_INVALID_ARG;
   if (tokens == 0) return CSD_OK;
+  // no two values of out at one place: one of the two axes lies within a step of the other
+  const auto within = [&](int64_t few, int64_t near, int64_t many, int64_t far) {
+    return (few == 1 || near >= head_dim) && (many == 1 || far >= (few - 1) * near + head_dim);
+  };
+  if (!within(heads, out->head_stride, tokens, out->token_stride) && !within(tokens, out->token_stride, heads, out->head_stride)) return CSD_ERR_INVALID_ARG;
   const int64_t groups = (tokens + kGroup - 1) / kGroup;
   const int32_t per = heads_of_group(groups, heads);
   const RotateArgs a{*rotary, *x, *out, d_positions, tokens, heads, head_dim, per};

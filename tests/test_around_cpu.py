@@ -80,6 +80,13 @@ def test_arguments_of_a_rotation_that_are_refused(lib):
     assert lib.csd_rotate(None, None, None, 1, 1, 64, 0, None, None) == b.ERR_INVALID_ARG
 
 
+def test_results_of_a_rotation_at_one_place_are_refused(lib):
+    how, x = verify.RotaryConfig(4096, 64, 0, 1.0), verify.Heads(4096, 0, 0, 0)                       # (what is read may be)
+    for token, head in ((0, 64), (512, 0), (512, 56), (504, 64), (64, 128), (56, 192), (64, 184)):
+        out = verify.Heads(1 << 20, 0, token, head)
+        assert lib.csd_rotate(ctypes.byref(how), ctypes.byref(x), 4096, 3, 8, 64, 0, ctypes.byref(out), None) == b.ERR_INVALID_ARG, (token, head)
+
+
 def test_arguments_of_attention_of_prompts_that_are_refused(lib):
     good = dict(q=4096, k=8192, v=16384, stride=512, head=64, type=0, n_heads=8, n_kv_heads=2, head_dim=64, offsets=4096, sequences=2, tokens=10, scale=0.1, out=4096, lse=None)
 

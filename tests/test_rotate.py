@@ -206,3 +206,14 @@ def test_arguments_that_are_refused(gen):
     ]:
         with pytest.raises(error):
             call()
+
+
+def test_results_at_one_place_are_refused(gen):
+    x, at, rotary = normal(gen, (6, 4, 64), BF), torch.zeros(6, dtype=torch.int32, device="cuda"), verify.Rotary(64)
+    same_for_all = x[:1].expand(6, 4, 64)
+    assert same(verify.rotate(same_for_all, at, rotary), same_for_all)                                  # read from one place
+    for out in (same_for_all, x[:, :1].expand(6, 4, 64), torch.empty(10000, dtype=BF, device="cuda").as_strided((6, 4, 64), (128, 64, 1))):
+        with pytest.raises(binding.CsdError):
+            verify.rotate(same_for_all if out is same_for_all else x[:, :1].expand(6, 4, 64) if out.stride(1) == 0 else x, at, rotary, out=out)
+    heads_first = torch.zeros((4, 6, 64), dtype=BF, device="cuda").transpose(0, 1)
+    assert same(verify.rotate(x, at, rotary, out=heads_first).contiguous(), x)
