@@ -203,7 +203,8 @@ int csd_cache_write_packed(csd_cache* cache, int32_t layer, const csd_heads* k, 
  *   d_lse    [tokens][n_heads] float = ln sum_x exp(scale * q.k_x), may be NULL
  * Tokens of no sequence are not written.  Nothing that a token does not see, not even an infinity or a NaN, changes its result; where
  * all that it sees weighs nothing (every score -inf), it gets zeros and -inf.
- * head_dim 64, 96, 128 or 256 (else CSD_ERR_UNIMPLEMENTED), type CSD_BF16 or CSD_F16; token strides of k and v up to 2^24 elements;
+ * head_dim 64, 96, 128 or 256 (else CSD_ERR_UNIMPLEMENTED), type CSD_BF16 or CSD_F16; scale finite, times log2 e too; token strides of k and v
+ * up to 2^24 elements;
  * (tokens * n_heads / n_kv_heads / 128 + sequences) * n_kv_heads up to 2^23. */
 int csd_prompt_attend(const csd_heads* q, const csd_heads* k, const csd_heads* v, int32_t type, int32_t n_heads, int32_t n_kv_heads,
                       int32_t head_dim, const int32_t* d_offsets, int32_t sequences, int64_t tokens, float scale, void* d_out, float* d_lse,

@@ -17,10 +17,10 @@ struct PromptArgs {
 
 constexpr int kPromptTile = 2 * kBlock, kPromptStages = 2;
 
-// The item of a workgroup: a tile of `wide` rows of a sequence, for a kv head.  Of up to 64 sequences the longest go first, each from its last tile
+// The item of a workgroup: a tile of `wide` rows of a sequence, for a kv head.  Of up to kSorted sequences the longest go first, each from its last tile
 // (the longest run of tokens) on, so that no long item is left for the end, while the items at work at a time share their tokens.
 // false: there is none.
-constexpr int32_t kSorted = 16, kSortedItems = 3072;
+constexpr int32_t kSorted = 16, kSortedItems = 12 * 256;
 __device__ inline bool sorted_item(const PromptArgs& a, uint32_t block, int32_t wide, bool pairs, Sequence* seq, int32_t* head) {
   const int32_t lane = threadIdx.x & 63;
   const auto offset = [&](int32_t i) {

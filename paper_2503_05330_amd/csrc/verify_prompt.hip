@@ -7,8 +7,9 @@ extern "C" int csd_prompt_attend(const csd_heads* q, const csd_heads* k, const c
                                  int32_t head_dim, const int32_t* d_offsets, int32_t sequences, int64_t tokens, float scale, void* d_out, float* d_lse,
                                  void* stream) {
   using namespace csd::verify;
+  constexpr float kLog2E = 1.44269504088896340736f;
   if (n_kv_heads <= 0 || n_heads <= 0 || n_heads > CSD_MAX_HEADS || n_heads % n_kv_heads || head_dim <= 0) return CSD_ERR_INVALID_ARG;
-  if ((type != CSD_BF16 && type != CSD_F16) || sequences <= 0 || sequences > CSD_MAX_SEQUENCES || tokens < 0 || tokens > CSD_MAX_PACKED_TOKENS || !std::isfinite(scale))
+  if ((type != CSD_BF16 && type != CSD_F16) || sequences <= 0 || sequences > CSD_MAX_SEQUENCES || tokens < 0 || tokens > CSD_MAX_PACKED_TOKENS || !std::isfinite(scale * kLog2E))
     return CSD_ERR_INVALID_ARG;
   auto bad = [](const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; };
   for (const csd_heads* h : {q, k, v})
@@ -21,7 +22,7 @@ extern "C" int csd_prompt_attend(const csd_heads* q, const csd_heads* k, const c
   const int64_t tiles = tokens * G / 128 + sequences;
   if (tiles * n_kv_heads > 1 << 23) return CSD_ERR_INVALID_ARG;
   if (tokens == 0) return CSD_OK;
-  const PromptArgs a{*q, *k, *v, d_offsets, sequences, (int32_t)tokens, n_kv_heads, G, (int32_t)tiles, scale * 1.44269504088896340736f, d_out, d_lse};
+  const PromptArgs a{*q, *k, *v, d_offsets, sequences, (int32_t)tokens, n_kv_heads, G, (int32_t)tiles, scale * kLog2E, d_out, d_lse};
   hipStream_t st = static_cast<hipStream_t>(stream);
   switch (head_dim) {
     case 64: prompt_64(a, type == CSD_F16, st); break;

@@ -256,8 +256,9 @@ class PathCache:
         int32, ascending), which become its prompt, from position 0 on."""
         c = self.cfg
         kh, vh = (_packed(t, self.dtype, c.n_kv_heads, c.head_dim) for t in (k, v))
-        if v.shape != k.shape:
+        if v.shape != k.shape or k.dim() != 3:
             raise ValueError("keys of shape %s, values of shape %s" % (tuple(k.shape), tuple(v.shape)))
+        _here(offsets)
         _check(load().csd_cache_write_packed(self._h, layer, ctypes.byref(kh), ctypes.byref(vh), _ptr(offsets, torch.int32, self.P + 1),
                                              len(k), _stream()), "csd_cache_write_packed")
 

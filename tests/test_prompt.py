@@ -268,3 +268,16 @@ def test_arguments_that_are_refused(gen):
             call()
     with torch.no_grad():
         verify.prompt_attend(wants(q), k, k, offsets)
+
+
+def test_packed_keys_of_more_axes_are_refused(gen):
+    c, k = verify.PathCache(1, 1, 16, 1, 8, 2, 64, 1), normal(gen, (2, 5, 2, 64), BF)
+    with pytest.raises(ValueError):                                                                     # (whose length is not that of the tokens)
+        c.write_packed(0, k, k, ints([0, 10]))
+
+
+def test_scales_beyond_32_bits_are_refused(gen):
+    q, k = normal(gen, (3, 2, 64), BF), normal(gen, (3, 2, 64), BF)
+    for scale in (3e38, -3e38):                                                                         # (times log2 e)
+        with pytest.raises(binding.CsdError):
+            verify.prompt_attend(q, k, k, ints([0, 3]), scale=scale)
