@@ -5,7 +5,8 @@
 // which is the launch).
 //
 // The calls of verify.py likewise (us a call from a loop, in Python and here: write() 9.0 and 4.1, read()
-// 9.7 and 5.9, targets() 11.7 and 7.3 where its kernel takes 7; attend() 10.4 and 9.3, its kernel).
+// 9.7 and 5.9, targets() 11.7 and 7.3 where its kernel takes 7; attend() 10.4 and 9.3, its kernel;
+// rotate() 15.9 and 5.6, write_rotated() 16.2 and 6.2, prompt_attend() 21.2 and 5.5, adjust() 17.5 and 5.5).
 //
 // Every function returns None where an argument is not what the call usually gets (another type,
 // a tensor of another kind): binding.py then goes its own way, which raises the error or serves it.

@@ -1,4 +1,21 @@
 // csd — attention of packed sequences to themselves: its kernel.
+//
+// Token t of a sequence sees its tokens 0 .. t: out = sum_x softmax_x(scale q.k_x) v_x.  The G query heads of a kv head make G rows of a
+// token, rows of a sequence lie behind each other (row = token * G + g), and a workgroup takes a tile of them for a kv head: what it
+// loads of keys and values serves all G heads.  A wave has 32 rows, in the orientation of csd_attend.cuh: S^T = K Q^T and O^T += V^T P^T
+// with a running (near) maximum and sum, no weight leaving its lane.  Keys and values come in tiles of 64 tokens to a ring of two in
+// LDS, by loads that pass no register, the next tile's during the products of one; all waves of the workgroup read the same.
+// Tiles that all rows see whole come first, without a mask; the last few, of which rows see a part, are edge()'s.
+//
+// What bounds it: at length power, then LDS.  One sequence of 16384 tokens, 28 heads of 128 on 4: 1.66 .. 1.74 ms, 1100 .. 1160 TFLOP/s (a product
+// of 16384^3 reaches 1360; this kernel 1460 with operands of zeros, at which the clock stays up).  8 x 4096, 32 on 8: 1.05 ms, 1050.  A wave's operands from
+// LDS, 32 rows a wave, take about as long as the products.  64 rows a wave, half of these reads, leave one wave a SIMD: its accumulators move
+// between register files, 1.78 us a tile of 256 rows for 1.5, and 25 us before and behind.  Short ones are bound by what comes one after the
+// other: 0.75 us a tile of 64 tokens for a workgroup, 6.5 us of launch, first loads and results; 5 x 777 tokens 14.6 us,
+// 16 sequences of 1024 down to 1 token 78 (35 at the rate of a large product).
+//
+// Scores of the next tile before the softmax of one, which would keep the matrix cores busy with one wave, spill; with two waves a SIMD the other
+// does that.  Four tiles in LDS instead of two leave one workgroup a CU, and gained nothing.
 #pragma once
 
 #include "csd_attend_rows.cuh"
@@ -365,6 +382,10 @@ void prompt_as(PromptArgs a, hipStream_t st) {
   a.tiles = (int32_t)((int64_t)a.tokens * a.G / (32 * WAVES) + a.sequences);
   prompt_kernel<T, D, WAVES><<<(uint32_t)a.tiles * (uint32_t)a.Hk, 64 * WAVES, kPromptStages * PromptWave<T, D>::kStage, st>>>(a);
 }
+// Eight waves share what four would load each, in tiles of 256 rows instead of 128: worth it where there are two such workgroups a CU at least and
+// sequences are long beside a tile.  8192 tokens of 16 heads of 128: 253 us with eight, 279 with four; 8 x 4096, 32 on 8: 1057 and 1073.  Else a
+// tile's last part is wasted and the longest item is longer: 16 sequences of 1 .. 1024 tokens 92 and 83, one of 2048 55 and 48.  Heads of 64 load
+// little (4 x 8192 672 and 629), those of 256 have no room.
 template <class T, int D>
 void prompt_of(const PromptArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.tokens * a.G;
