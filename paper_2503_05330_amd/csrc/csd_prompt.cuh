@@ -38,7 +38,9 @@ constexpr int kPromptTile = 2 * kBlock, kPromptStages = 2;
 // its place, of the sequence's last token (`left`: its tokens from the tile's first on) where there is none.
 template <class R, int WAVES>
 struct TileLoads {
-  static constexpr int kPieces = 2 * R::kPieces / WAVES, kApart = 64 * WAVES / R::kChunks;       // piece wave + WAVES x; tokens from one to the next
+  static constexpr int kAll = 2 * R::kPieces, kPieces = (kAll + WAVES - 1) / WAVES;              // piece wave + WAVES x, where it is one of all
+  static constexpr int kApart = 64 * WAVES / R::kChunks;                                         // tokens from one to the next
+  static __device__ bool there(int x, int wave) { return kAll % WAVES == 0 || wave + WAVES * x < kAll; }
   static constexpr bool kAlike = R::kSwizzled;           // the lane's places in its pieces differ by whole tokens and a constant order of chunks
   uint32_t at[kAlike ? 1 : kPieces];
   static __device__ uint32_t place(int x, int64_t stride, int32_t left, int wave, int lane) {
@@ -54,6 +56,7 @@ struct TileLoads {
   __device__ void fetch_to(uint32_t lds, const One* from, int64_t stride, int wave) const {
 #pragma unroll
     for (int x = 0; x < kPieces; ++x) {
+      if (!there(x, wave)) continue;
       const uint32_t to = uniform(lds + 1024u * (WAVES * x + wave));
       if constexpr (kAlike) fetch(to, uniform(reinterpret_cast<const uint8_t*>(from + x * kApart * stride)), at[0] ^ R::swizzle(x * kApart & 31) << 4);
       else fetch(to, uniform(reinterpret_cast<const uint8_t*>(from)), at[x]);
@@ -63,7 +66,7 @@ struct TileLoads {
   static __device__ void fetch_part(uint32_t lds, const One* from, int64_t stride, int32_t left, int wave, int lane) {
 #pragma unroll
     for (int x = 0; x < kPieces; ++x)
-      fetch(uniform(lds + 1024u * (WAVES * x + wave)), uniform(reinterpret_cast<const uint8_t*>(from)), place(x, stride, left, wave, lane));
+      if (there(x, wave)) fetch(uniform(lds + 1024u * (WAVES * x + wave)), uniform(reinterpret_cast<const uint8_t*>(from)), place(x, stride, left, wave, lane));
   }
 };
 

@@ -281,3 +281,13 @@ def test_scales_beyond_32_bits_are_refused(gen):
     for scale in (3e38, -3e38):                                                                         # (times log2 e)
         with pytest.raises(binding.CsdError):
             verify.prompt_attend(q, k, k, ints([0, 3]), scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [BF, F16])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("lengths,H,Hk", [([261], 512, 8), ([259, 262], 512, 8), ([1100], 128, 32)])
+def test_launches_that_fill_the_chip(gen, lengths, H, Hk, D, dtype):
+    """(more than 512 tiles of 256 rows, of 4096 rows a sequence and more: the largest workgroups)"""
+    rows = sum(lengths) * H // Hk
+    assert rows >= 4096 * len(lengths) and rows // 256 * Hk >= 512
+    check(gen, lengths, H, Hk, D, dtype=dtype)
