@@ -290,15 +290,16 @@ struct PromptWave {
   }
 };
 
-template <class T, int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D <= 128 ? 2 : 1) void prompt_kernel(PromptArgs a) {
-  constexpr int kPromptRows = 32 * WAVES;
+// PARTS waves share a row's tiles in turn and add up what they have at the end.
+template <class T, int D, int ROW_WAVES, int PARTS>
+__global__ __launch_bounds__(64 * ROW_WAVES * PARTS, D <= 128 ? 2 : 1) void prompt_kernel(PromptArgs a) {
+  constexpr int WAVES = ROW_WAVES * PARTS, kPromptRows = 32 * ROW_WAVES;
   typedef typename T::One One;
   typedef typename T::Eight Eight;
   typedef Rows<D, false> R;
-  constexpr int kStage = PromptWave<T, D>::kStage;
+  constexpr int kTileBytes = PromptWave<T, D>::kStage, kStage = kTileBytes * PARTS;
   extern __shared__ __align__(512) uint8_t ring[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row_wave = wave % ROW_WAVES, part = wave / ROW_WAVES;
   // A sequence's last tiles, the longest runs of tokens, go first.  (Sequences in order of their lengths too, the longest ones first: 16 of 32 .. 1024
   // tokens 76 us for 78, 16 of 256 30 for 28, one of 4096 before or behind seven of 1000 214 for 208 and 213 for 212.)
   const int32_t head = blockIdx.x % (uint32_t)a.Hk;
@@ -307,11 +308,11 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 ? 2 : 1) void prompt_kernel(Pr
   if (first >= rows) return;
   const int32_t here = rows - first < kPromptRows ? (int32_t)(rows - first) : kPromptRows;
 
-  const uint32_t lds = uniform(lds_offset(ring));
+  const uint32_t lds = uniform(lds_offset(ring)), lds_own = lds + part * kTileBytes;
   PromptWave<T, D> p;
   auto& w = p.w;
-  p.begin(a.scale, lds);
-  const int32_t own = 32 * wave + (lane & 31);
+  p.begin(a.scale, lds_own);
+  const int32_t own = 32 * row_wave + (lane & 31);
   const bool valid = own < here;
   const int32_t token = (int32_t)((first + (valid ? own : 0)) / a.G), g = (int32_t)(first + (valid ? own : 0) - (int64_t)token * a.G);
   const int32_t sees = valid ? token + 1 : 0;
@@ -327,18 +328,18 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 ? 2 : 1) void prompt_kernel(Pr
     }
   };
   // what all and what any of the wave's, of the workgroup's rows see
-  const int32_t wave_here = here - 32 * wave;
-  const int32_t all = wave_here > 0 ? (int32_t)((first + 32 * wave) / a.G) + 1 : 0;
-  const int32_t most = wave_here > 0 ? (int32_t)((first + 32 * wave + (wave_here < 32 ? wave_here : 32) - 1) / a.G) + 1 : 0;
+  const int32_t wave_here = here - 32 * row_wave;
+  const int32_t all = wave_here > 0 ? (int32_t)((first + 32 * row_wave) / a.G) + 1 : 0;
+  const int32_t most = wave_here > 0 ? (int32_t)((first + 32 * row_wave + (wave_here < 32 ? wave_here : 32) - 1) / a.G) + 1 : 0;
   const int32_t end = (int32_t)((first + here - 1) / a.G) + 1;
-  const int32_t tiles = (end + kPromptTile - 1) / kPromptTile;
+  const int32_t tiles = (end + kPromptTile - 1) / kPromptTile, steps = (tiles + PARTS - 1) / PARTS;
 
   const One* const keys = static_cast<const One*>(a.k.data) + seq.from * a.k.token_stride + head * a.k.head_stride;
   const One* const values = static_cast<const One*>(a.v.data) + seq.from * a.v.token_stride + head * a.v.head_stride;
   typedef TileLoads<R, WAVES> Loads;
   const Loads of_keys(a.k.token_stride, wave, lane), of_values(a.v.token_stride, wave, lane);
   // (the wave has read what lies in the stage: it waits for its reads before the barrier that all loads stand behind)
-  const auto load = [&](int32_t tile, uint32_t to) {
+  const auto load_tile = [&](int32_t tile, uint32_t to) {
     const int32_t left = seq.length - tile * kPromptTile;
     const One* const k = keys + (int64_t)tile * kPromptTile * a.k.token_stride;
     const One* const v = values + (int64_t)tile * kPromptTile * a.v.token_stride;
@@ -350,15 +351,20 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 ? 2 : 1) void prompt_kernel(Pr
       Loads::fetch_part(lds + to + 2 * R::kHalf, v, a.v.token_stride, left, wave, lane);
     }
   };
+  const auto load = [&](int32_t step, uint32_t to) {
+#pragma unroll
+    for (int x = 0; x < PARTS; ++x)
+      if (x == 0 || step * PARTS + x < tiles) load_tile(step * PARTS + x, to + x * kTileBytes);
+  };
   load(0, 0);
   queries();
   __builtin_amdgcn_s_waitcnt(0x0f70);                    // vmcnt(0), with the builtin, so that the compiler knows and does not wait for the queries in the loop
   const auto next = [&](int32_t j, uint32_t at) {
     wait_loads<0>();
     meet();                                              // the tile is there, and all are done with the one before
-    if (j + 1 < tiles) load(j + 1, at ^ kStage);
+    if (j + 1 < steps) load(j + 1, at ^ kStage);
   };
-  const int32_t whole = all / kPromptTile < tiles ? all / kPromptTile : tiles;
+  const int32_t whole = (all / kPromptTile - part + PARTS - 1) / PARTS;    // steps (all / kPromptTile: at most tiles)
   int32_t j = 0;
   for (; j + 2 <= whole; j += 2) {
     next(j, 0);
@@ -370,32 +376,69 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 ? 2 : 1) void prompt_kernel(Pr
     next(j++, 0);
     p.whole(0);
   }
-  for (; j < tiles; ++j) {
+  for (; j < steps; ++j) {
     const uint32_t at = j % 2 * kStage;
     next(j, at);
-    const int32_t from = j * kPromptTile;
-    if (most > from) p.edge(lds, at, sees - from, most - from);
+    const int32_t from = (j * PARTS + part) * kPromptTile;
+    if (most > from) p.edge(lds_own, at, sees - from, most - from);
   }
 
+  if constexpr (PARTS == 2) {
+    constexpr int kNumbers = D / 2 + 2;                  // of a lane
+    static_assert(kNumbers * 64 * 4 * ROW_WAVES <= kPromptStages * kStage, "");
+    float* const other = reinterpret_cast<float*>(ring) + row_wave * 64 * kNumbers + lane;
+    __syncthreads();
+    if (part == 1) {
+#pragma unroll
+      for (int i = 0; i < D / 2; ++i) other[64 * i] = w.o[i / 16][i % 16];
+      other[64 * (D / 2)] = w.l;
+      other[64 * (D / 2 + 1)] = w.m;
+    }
+    __syncthreads();
+    if (part == 1) return;
+    const float m = other[64 * (D / 2 + 1)], high = fmaxf(w.m, m);
+    const float mine = w.m == kNone ? 0.0f : exp2_fast(w.m - high), its = m == kNone ? 0.0f : exp2_fast(m - high);
+    w.m = high;
+    w.l = w.l * mine + other[64 * (D / 2)] * its;
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) w.o[i / 16][i % 16] = w.o[i / 16][i % 16] * mine + other[64 * i] * its;
+  }
   write_row<T, D>(a, w.o, w.m, w.l, at * a.Hk * a.G + head * a.G + g, valid, w.half);
 }
 
-template <class T, int D, int WAVES>
+template <class T, int D, int ROW_WAVES, int PARTS>
 void prompt_as(PromptArgs a, hipStream_t st) {
-  a.tiles = (int32_t)((int64_t)a.tokens * a.G / (32 * WAVES) + a.sequences);
-  prompt_kernel<T, D, WAVES><<<(uint32_t)a.tiles * (uint32_t)a.Hk, 64 * WAVES, kPromptStages * PromptWave<T, D>::kStage, st>>>(a);
+  a.tiles = (int32_t)((int64_t)a.tokens * a.G / (32 * ROW_WAVES) + a.sequences);
+  prompt_kernel<T, D, ROW_WAVES, PARTS><<<(uint32_t)a.tiles * (uint32_t)a.Hk, 64 * ROW_WAVES * PARTS, kPromptStages * PARTS * PromptWave<T, D>::kStage, st>>>(a);
 }
-// Eight waves share what four would load each, in tiles of 256 rows instead of 128: worth it where there are two such workgroups a CU at least and
-// sequences are long beside a tile.  8192 tokens of 16 heads of 128: 253 us with eight, 279 with four; 8 x 4096, 32 on 8: 1057 and 1073.  Else a
-// tile's last part is wasted and the longest item is longer: 16 sequences of 1 .. 1024 tokens 92 and 83, one of 2048 55 and 48.  Heads of 64 load
-// little (4 x 8192 672 and 629), those of 256 have no room.
+// The workgroup of a launch, by the items (tiles of rows, kv heads) that it has at most.
+//
+// Eight waves of rows share what four would load each: worth it where there are two such workgroups a CU at least and sequences are long beside a
+// tile of 256 rows.  8192 tokens of 16 heads of 128: 253 us with eight, 279 with four; 8 x 4096, 32 on 8: 1057 and 1073.  Else a tile's last
+// part is wasted and the longest item is longer: 16 sequences of 1 .. 1024 tokens 92 and 83, one of 2048 55 and 48.  Heads of 64 load little (4 x
+// 8192 672 and 629), those of 256 have no room.
+//
+// Where four waves of rows leave CUs without work, or with one wave a SIMD, two waves share each row's tokens: the time is that of the longest run
+// of tiles.  Tiles of 64 rows, while there is about one a CU (heads of 64: two, which LDS has room for); us, with four waves of 128
+// rows: 2048 tokens of 8 heads of 64 18.0 (27.8), 16 19.8 (28.1), 24 25.7 (28.7), 4 x 512 of 16 10.6 (12.9), 20 14.1 (13.7); of 8 heads of 128 27.1
+// (38.8), 4 x 512 of 8 11.9 (15.2), 12 20.2 (15.9).  Then tiles of 128 rows: 2048 tokens of 16 heads of 128 33.8 (39.6), 24 38.7 (43.2),
+// 4 x 512 of 16 16.1 (17.9), 20 25.6 (20.7).  (Sequences of 70 tokens: 7.2 for 6.9; of 100: 7.3 for 7.9.)
 template <class T, int D>
 void prompt_of(const PromptArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.tokens * a.G;
+  const auto items = [&](int64_t wide) { return (rows / wide + a.sequences) * a.Hk; };
   if constexpr (D == 96 || D == 128) {
-    if (rows >= 4096 * (int64_t)a.sequences && rows / 256 * a.Hk >= 512) return prompt_as<T, D, 8>(a, st);
+    if (rows >= 4096 * (int64_t)a.sequences && rows / 256 * a.Hk >= 512) return prompt_as<T, D, 8, 1>(a, st);
   }
-  prompt_as<T, D, 4>(a, st);
+  if constexpr (D <= 128) {
+    if (2 * (int64_t)a.tokens >= 3 * kPromptTile * (int64_t)a.sequences) {
+      if (items(64) <= (D == 64 ? 640 : 320)) return prompt_as<T, D, 2, 2>(a, st);
+      if constexpr (D > 64) {
+        if (items(128) <= 336) return prompt_as<T, D, 4, 2>(a, st);
+      }
+    }
+  }
+  prompt_as<T, D, 4, 1>(a, st);
 }
 template <int D>
 void prompt_of(const PromptArgs& a, bool f16, hipStream_t st) {

@@ -291,3 +291,43 @@ def test_launches_that_fill_the_chip(gen, lengths, H, Hk, D, dtype):
     rows = sum(lengths) * H // Hk
     assert rows >= 4096 * len(lengths) and rows // 256 * Hk >= 512
     check(gen, lengths, H, Hk, D, dtype=dtype)
+
+
+# kv heads and heads of each that take sequences of 200 and 60 tokens through every kind of workgroup
+FORMS = [(2, 4), (64, 1), (128, 1), (16, 32)]
+
+
+@pytest.mark.parametrize("dtype", [BF, F16])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("Hk,G", FORMS)
+def test_every_workgroup_with_odd_tokens(gen, Hk, G, D, dtype):
+    def poison(q, k, v):
+        v[35, :, 3], k[150, :, 5] = float("nan"), float("nan")
+        v[31, :, 0], v[100, :, 1], v[130, :, D - 1] = float("inf"), float("-inf"), float("inf")
+        v[199], k[199] = float("nan"), float("nan")
+    print(Hk, G, D, dtype, flush=True)
+    *_, out = check(gen, [200, 60], Hk * G, Hk, D, dtype=dtype, poison=poison, behind=20)
+    assert out[:150].isfinite()[:, :, 2].all() and out[200:260].isfinite().all()
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("Hk,G", FORMS)
+def test_every_workgroup_with_tokens_that_weigh_nothing(gen, Hk, G, D):
+    """Scores of -inf for all that a wave sees, of some rows and of all."""
+    T, H = 270, Hk * G
+    q, k, v = torch.zeros((T, H, D), dtype=BF, device="cuda"), torch.zeros((T, Hk, D), dtype=BF, device="cuda"), normal(gen, (T, Hk, D), BF)
+    q[..., 0] = 1
+    counts = torch.ones(T, dtype=torch.bool, device="cuda")
+    counts[:70] = counts[128:192] = counts[200:210] = False
+    k[~counts, :, 0] = -torch.inf
+    lse = torch.zeros((T, H), device="cuda")
+    out = verify.prompt_attend(q, k, v, ints([0, 210, T]), 1.0, lse=lse)
+    for a, b in ((0, 210), (210, T)):
+        n = counts[a:b].double().cumsum(0)
+        x = torch.where(counts[a:b, None, None], v[a:b].double(), 0.0)
+        # weights of one, exact; sums in 32 bits; one rounding
+        want, error = x.cumsum(0) / n.clamp(min=1)[:, None, None], x.abs().cumsum(0) * 280 * 2.0 ** -24 / n.clamp(min=1)[:, None, None]
+        want, error = (t.repeat_interleave(G, 1) for t in (want, error + ROUND[BF] * want.abs()))
+        assert ((out[a:b].double() - want).abs() <= error * (1 + 2.0 ** -7)).all()
+        assert ((lse[a:b].double() - n.log()[:, None]).abs()[n > 0] <= 2.0 ** -20 * 6).all() and (lse[a:b][n == 0] == -torch.inf).all()
+    assert not out[:70].any()
