@@ -11,8 +11,8 @@
 // of 16384^3 reaches 1360; this kernel 1460 with operands of zeros, at which the clock stays up).  8 x 4096, 32 on 8: 1.05 ms, 1050.  A wave's operands from
 // LDS, 32 rows a wave, take about as long as the products.  64 rows a wave, half of these reads, leave one wave a SIMD: its accumulators move
 // between register files, 1.78 us a tile of 256 rows for 1.5, and 25 us before and behind.  Short ones are bound by what comes one after the
-// other: 0.75 us a tile of 64 tokens for a workgroup, 6.5 us of launch, first loads and results; 5 x 777 tokens 14.6 us,
-// 16 sequences of 1024 down to 1 token 78 (35 at the rate of a large product).
+// other: 0.75 .. 0.95 us a tile of 64 tokens for a wave, 6.5 us of launch, first loads and results.  5 sequences of 331 .. 777 tokens, 12 heads of 64:
+// 13.1 us; 16 of 1 .. 1024, 32 on 8 of 128: 75 .. 81 (35 at the rate of a large product).
 //
 // Scores of the next tile before the softmax of one, which would keep the matrix cores busy with one wave, spill; with two waves a SIMD the other
 // does that.  Four tiles in LDS instead of two leave one workgroup a CU, and gained nothing.
@@ -415,8 +415,8 @@ void prompt_as(PromptArgs a, hipStream_t st) {
 //
 // Eight waves of rows share what four would load each: worth it where there are two such workgroups a CU at least and sequences are long beside a
 // tile of 256 rows.  8192 tokens of 16 heads of 128: 253 us with eight, 279 with four; 8 x 4096, 32 on 8: 1057 and 1073.  Else a tile's last
-// part is wasted and the longest item is longer: 16 sequences of 1 .. 1024 tokens 92 and 83, one of 2048 55 and 48.  Heads of 64 load little (4 x
-// 8192 672 and 629), those of 256 have no room.
+// part is wasted and the longest item is longer: 16 sequences of 1 .. 1024 tokens 92 and 83, one of 2048 55 and 48.  Heads of 64 and 96
+// load little (4 x 8192 of 16 of 64 672 and 629, 8192 of 32 on 8 of 96 471 and 470), those of 256 have no room.
 //
 // Where four waves of rows leave CUs without work, or with one wave a SIMD, two waves share each row's tokens: the time is that of the longest run
 // of tiles.  Tiles of 64 rows, while there is about one a CU (heads of 64: two, which LDS has room for); us, with four waves of 128
@@ -427,7 +427,7 @@ template <class T, int D>
 void prompt_of(const PromptArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.tokens * a.G;
   const auto items = [&](int64_t wide) { return (rows / wide + a.sequences) * a.Hk; };
-  if constexpr (D == 96 || D == 128) {
+  if constexpr (D == 128) {
     if (rows >= 4096 * (int64_t)a.sequences && rows / 256 * a.Hk >= 512) return prompt_as<T, D, 8, 1>(a, st);
   }
   if constexpr (D <= 128) {
