@@ -18,7 +18,7 @@ namespace {
 
 constexpr uint32_t kNew = 1u << 30, kPrompt = 1u << 31;
 
-constexpr int kThreads = 512;                            // (256 .. 1024: no faster)
+constexpr int kAdjustThreads = 512;                            // (256 .. 1024: no faster)
 
 // Tokens that the workgroup looks at: the first few of each thread are asked for at once, so that they are on their way together with all else.
 struct Tokens {
@@ -30,7 +30,7 @@ struct Tokens {
   __device__ void ask(Four (&x)[kAhead], int32_t x0) const {
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
-      const int32_t at = x0 + s * kThreads;
+      const int32_t at = x0 + s * kAdjustThreads;
       x[s] = 4 * at + 3 < length ? *reinterpret_cast<const Four*>(from + 4 * at) : Four{};
     }
   }
@@ -42,11 +42,11 @@ struct Tokens {
     Four x[kAhead];
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) x[s] = first[s];
-    for (int32_t x0 = threadIdx.x; x0 < fours; x0 += kAhead * kThreads) {
+    for (int32_t x0 = threadIdx.x; x0 < fours; x0 += kAhead * kAdjustThreads) {
       if (x0 != (int32_t)threadIdx.x) ask(x, x0);
 #pragma unroll
       for (int s = 0; s < kAhead; ++s) {
-        if (x0 + s * kThreads >= fours) break;
+        if (x0 + s * kAdjustThreads >= fours) break;
 #pragma unroll
         for (int i = 0; i < 4; ++i) f((uint32_t)x[s][i]);
       }
@@ -56,7 +56,7 @@ struct Tokens {
 };
 
 template <class E>
-__global__ __launch_bounds__(kThreads) void adjust_kernel(csd_adjustment a, int32_t first_path, int32_t parts, int32_t per) {
+__global__ __launch_bounds__(kAdjustThreads) void adjust_kernel(csd_adjustment a, int32_t first_path, int32_t parts, int32_t per) {
   extern __shared__ __align__(32) uint32_t words[];      // of the stretch's tokens
   __shared__ int32_t newest[CSD_MAX_VERIFY_STEP];
   const int32_t path = first_path + blockIdx.x / (uint32_t)parts, part = blockIdx.x % (uint32_t)parts, p = path / a.n_paths;
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(csd_adjustment a, int3
   const auto ask = [&](int32_t x0) {
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
-      const int32_t item = x0 + s * kThreads < all ? x0 + s * kThreads : x0;
+      const int32_t item = x0 + s * kAdjustThreads < all ? x0 + s * kAdjustThreads : x0;
       t[s] = item / eights;
       at[s] = 8 * (item - t[s] * eights);
       x[s] = *reinterpret_cast<const Eight*>(in + t[s] * a.logit_stride + at[s]);
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(csd_adjustment a, int3
     repetition = a.d_penalties[3 * (int64_t)p];
     presence = a.d_penalties[3 * (int64_t)p + 1];
     frequency = a.d_penalties[3 * (int64_t)p + 2];
-    for (int32_t x = threadIdx.x; x < per / 4; x += kThreads) reinterpret_cast<uint4*>(words)[x] = uint4{};
+    for (int32_t x = threadIdx.x; x < per / 4; x += kAdjustThreads) reinterpret_cast<uint4*>(words)[x] = uint4{};
     if (threadIdx.x < CSD_MAX_VERIFY_STEP) {
       const int32_t at = before + (int32_t)threadIdx.x;
       newest[threadIdx.x] = said && (int32_t)threadIdx.x < count && at >= 0 ? said[at] : -1;
@@ -140,11 +140,11 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(csd_adjustment a, int3
     if (times) y -= frequency * (float)times + presence;
     return y;
   };
-  for (int32_t x0 = threadIdx.x; x0 < all; x0 += kAhead * kThreads) {
+  for (int32_t x0 = threadIdx.x; x0 < all; x0 += kAhead * kAdjustThreads) {
     if (x0 != (int32_t)threadIdx.x) ask(x0);
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
-      if (x0 + s * kThreads >= all) break;
+      if (x0 + s * kAdjustThreads >= all) break;
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = (float)x[s][i];
@@ -175,12 +175,12 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(csd_adjustment a, int3
     out[t * a.out_stride + at] = (E)(allowed(t, eights * 8) >> i & 1 ? y : -INFINITY);
   }
   for (int32_t t = count; t < a.n; ++t) {
-    for (int32_t x = threadIdx.x; x < eights; x += kThreads) *reinterpret_cast<Eight*>(out + t * a.out_stride + 8 * x) = Eight{};
+    for (int32_t x = threadIdx.x; x < eights; x += kAdjustThreads) *reinterpret_cast<Eight*>(out + t * a.out_stride + 8 * x) = Eight{};
     if ((int32_t)threadIdx.x < rest) out[t * a.out_stride + eights * 8 + threadIdx.x] = (E)0.0f;
   }
 }
 
-constexpr int32_t kLeastLogits = 1024;
+constexpr int32_t kLeastStretch = 1024;
 
 }  // namespace
 }  // namespace verify
@@ -209,7 +209,7 @@ extern "C" int csd_adjust(const csd_adjustment* adjustment, void* stream) {
   // paths x 1 position 373, 261, 180; 256 x 4 141, 116, 114; 128 x 8 107, 110, 119; 64 x 17 117, 130, 146.
   const int32_t longest = a.n <= 4 ? 8192 : a.n < 8 ? 4096 : 2048;
   int64_t parts = (1024 + paths - 1) / paths;
-  const int64_t most = (a.vocab + kLeastLogits - 1) / kLeastLogits, least = (a.vocab + longest - 1) / longest;
+  const int64_t most = (a.vocab + kLeastStretch - 1) / kLeastStretch, least = (a.vocab + longest - 1) / longest;
   parts = parts < least ? least : parts > most ? most : parts;
   const int32_t per = (int32_t)(((a.vocab + parts - 1) / parts + 31) / 32 * 32);
   parts = (a.vocab + per - 1) / per;
@@ -218,7 +218,7 @@ extern "C" int csd_adjust(const csd_adjustment* adjustment, void* stream) {
   const int64_t together = ((int64_t)1 << 22) / parts;                // paths of a launch of less than 2^32 threads
   for (int64_t first = 0; first < paths; first += together) {
     const int64_t here = paths - first < together ? paths - first : together;
-    kernel<<<(uint32_t)(here * parts), kThreads, lds, static_cast<hipStream_t>(stream)>>>(a, (int32_t)first, (int32_t)parts, per);
+    kernel<<<(uint32_t)(here * parts), kAdjustThreads, lds, static_cast<hipStream_t>(stream)>>>(a, (int32_t)first, (int32_t)parts, per);
   }
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CSD_OK : csd::hip_fail(e, "csd_adjust");

@@ -14,7 +14,7 @@ namespace csd {
 namespace verify {
 namespace {
 
-constexpr int kThreads = 64 * kMoveWaves;
+constexpr int kRotateThreads = 64 * kMoveWaves;
 
 struct RotateArgs {
   csd_rotary how;
@@ -27,14 +27,14 @@ struct RotateArgs {
 // Eight tokens of `per` heads; a thread takes sixteen values of a token's head at a time, both eights of eight pairs (or, behind them, two
 // eights to be copied): two reads and two writes of 16 bytes, which the threads of a head and of the next ones do side by side.
 template <class T>
-__global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
+__global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs a) {
   typedef typename T::Eight Eight;
   typedef typename T::One Value;
   extern __shared__ Turn turns[];
   const int64_t first = (int64_t)blockIdx.x * kGroup;
   const int32_t here = a.tokens - first < kGroup ? (int32_t)(a.tokens - first) : kGroup;
   const int32_t pairs = a.how.dim / 2;
-  for (int32_t x = threadIdx.x; x < here * pairs; x += kThreads) {
+  for (int32_t x = threadIdx.x; x < here * pairs; x += kRotateThreads) {
     const int32_t token = x / pairs;
     Turns(turns, token, pairs)[x - token * pairs] = turn_of(a.how, a.positions[first + token], x - token * pairs);
   }
@@ -42,13 +42,13 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
   const int32_t head0 = blockIdx.y * a.per, heads = a.heads - head0 < a.per ? a.heads - head0 : a.per;
   const int32_t turning = a.how.dim / 16, units = turning + (a.dim - a.how.dim + 15) / 16, all = here * heads * units;
   constexpr int kAhead = 2;                              // (4: 133 us for 131 with 8 x 4096 tokens of 40 heads of 128; a copy of as much takes 130)
-  for (int32_t x0 = threadIdx.x; x0 < all; x0 += kAhead * kThreads) {
+  for (int32_t x0 = threadIdx.x; x0 < all; x0 += kAhead * kRotateThreads) {
     Eight u[kAhead], v[kAhead];
     int64_t to[kAhead];
     int32_t d[kAhead], e[kAhead], token[kAhead];         // where the two eights lie; e < 0: there is no second
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
-      const int32_t x = x0 + s * kThreads < all ? x0 + s * kThreads : x0;
+      const int32_t x = x0 + s * kRotateThreads < all ? x0 + s * kRotateThreads : x0;
       const int32_t row = x / units, unit = x - row * units;
       token[s] = row / heads;
       const int32_t head = head0 + row - token[s] * heads;
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
     }
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
-      if (x0 + s * kThreads >= all) break;
+      if (x0 + s * kRotateThreads >= all) break;
       Value* const out = static_cast<Value*>(const_cast<void*>(a.out.data)) + to[s];
       Eight y = u[s], z = v[s];
       if (d[s] < a.how.dim) {
@@ -101,7 +101,7 @@ struct PlaceArgs {
 
 // Eight tokens, of one path or of several; a wave takes a job of theirs at a time, eight lanes a token.
 template <class T, int D, bool FP8>
-__global__ __launch_bounds__(kThreads) void place_kernel(PlaceArgs a) {
+__global__ __launch_bounds__(kRotateThreads) void place_kernel(PlaceArgs a) {
   typedef typename T::Eight Eight;
   typedef typename T::One Value;
   typedef Pieces<D> P;
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(kThreads) void place_kernel(PlaceArgs a) {
   count = count > m.n ? m.n : count;
   const int64_t pos = (int64_t)(m.start ? m.start[row] : 0) + t;
   const bool asked = there && t < count, live = asked && pos >= 0 && pos < m.held.cap;
-  for (int32_t x = threadIdx.x; x < here * pairs; x += kThreads) {
+  for (int32_t x = threadIdx.x; x < here * pairs; x += kRotateThreads) {
     const int32_t of = x / pairs;
     Turns(turns, of, pairs)[x - of * pairs] = turn_of(a.how, a.positions[first + of], x - of * pairs);
   }
@@ -194,7 +194,7 @@ void cache_write_rotated(const MoveArgs& move, const csd_rotary& how, const csd_
     constexpr int D = dim();
     auto* kernel = f16 ? (fp8 ? place_kernel<F16, D, true> : place_kernel<F16, D, false>)
                        : (fp8 ? place_kernel<BF16, D, true> : place_kernel<BF16, D, false>);
-    kernel<<<grid, kThreads, 0, st>>>(a);
+    kernel<<<grid, kRotateThreads, 0, st>>>(a);
   });
 }
 
@@ -240,7 +240,7 @@ int csd_rotate(const csd_rotary* rotary, const csd_heads* x, const int32_t* d_po
   const RotateArgs a{*rotary, *x, *out, d_positions, tokens, heads, head_dim, per};
   const dim3 grid((uint32_t)groups, (uint32_t)((heads + per - 1) / per));
   auto* kernel = type == CSD_F16 ? rotate_kernel<F16> : rotate_kernel<BF16>;
-  kernel<<<grid, kThreads, Turns::size(kGroup, rotary->dim / 2) * sizeof(Turn), static_cast<hipStream_t>(stream)>>>(a);
+  kernel<<<grid, kRotateThreads, Turns::size(kGroup, rotary->dim / 2) * sizeof(Turn), static_cast<hipStream_t>(stream)>>>(a);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CSD_OK : csd::hip_fail(e, "csd_rotate");
 }
