@@ -170,18 +170,19 @@ struct PromptWave {
     }
   }
 
-  // A tile that all rows see whole, `at` in the ring.  Its values are read during the softmax.
+  // A tile that all rows see whole (BLOCKS of it), `at` in the ring.  Its values are read during the softmax.
+  template <int BLOCKS>
   __device__ void whole(uint32_t at) {
     Acc s[2];
-    scores<2>(s, at);
-    constexpr int kValues = 2 * kTiles, kValuesAhead = 4;
+    scores<BLOCKS>(s, at);
+    constexpr int kValues = BLOCKS * kTiles, kValuesAhead = kValues < 4 ? kValues : 4;
     Two v[kValuesAhead];
 #pragma unroll
     for (int i = 0; i < kValuesAhead; ++i) v[i] = value(at, i / kTiles, i % kTiles);
     __builtin_amdgcn_sched_barrier(0);
     float most = s[0][0];                                // (as in Wave::softmax)
 #pragma unroll
-    for (int i = 1; i < 32; ++i) most = fmaxf(most, s[i / 16][i % 16]);
+    for (int i = 1; i < 16 * BLOCKS; ++i) most = fmaxf(most, s[i / 16][i % 16]);
     most = both_max(most) * w.scale;
     if (__ballot(most > w.m + (W::kSlack + W::kLift))) {
       const float high = fmaxf(w.m, most - W::kLift), down = w.m == kNone ? 0.0f : exp2_fast(w.m - high);
@@ -204,7 +205,7 @@ struct PromptWave {
     weights(0);
     __builtin_amdgcn_sched_barrier(0);
     // the second block's weights go between the products of the first's
-    weights(1);
+    if constexpr (BLOCKS == 2) weights(1);
 #pragma unroll
     for (int i = 0; i < kValues; ++i) {
       const int e = i / kTiles, x = i % kTiles, next = i + kValuesAhead;
@@ -215,7 +216,7 @@ struct PromptWave {
 #pragma unroll
     for (int i = 0; i < 2 * kTiles; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 56 / (2 * kTiles), 0);
+      if constexpr (BLOCKS == 2) __builtin_amdgcn_sched_group_barrier(0x002, 56 / (2 * kTiles), 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -290,14 +291,14 @@ struct PromptWave {
   }
 };
 
-// PARTS waves share a row's tiles in turn and add up what they have at the end.
+// PARTS waves share a row, BLOCKS blocks of a tile's two each, and add up what they have at the end.
 template <class T, int D, int ROW_WAVES, int PARTS>
 __global__ __launch_bounds__(64 * ROW_WAVES * PARTS, D <= 128 ? 2 : 1) void prompt_kernel(PromptArgs a) {
   constexpr int WAVES = ROW_WAVES * PARTS, kPromptRows = 32 * ROW_WAVES;
   typedef typename T::One One;
   typedef typename T::Eight Eight;
   typedef Rows<D, false> R;
-  constexpr int kTileBytes = PromptWave<T, D>::kStage, kStage = kTileBytes * PARTS;
+  constexpr int kStage = PromptWave<T, D>::kStage, BLOCKS = 2 / PARTS, kOwn = BLOCKS * kBlock;
   extern __shared__ __align__(512) uint8_t ring[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row_wave = wave % ROW_WAVES, part = wave / ROW_WAVES;
   // A sequence's last tiles, the longest runs of tokens, go first.  (Sequences in order of their lengths too, the longest ones first: 16 of 32 .. 1024
@@ -308,7 +309,7 @@ __global__ __launch_bounds__(64 * ROW_WAVES * PARTS, D <= 128 ? 2 : 1) void prom
   if (first >= rows) return;
   const int32_t here = rows - first < kPromptRows ? (int32_t)(rows - first) : kPromptRows;
 
-  const uint32_t lds = uniform(lds_offset(ring)), lds_own = lds + part * kTileBytes;
+  const uint32_t lds = uniform(lds_offset(ring)), lds_own = lds + part * R::kHalf;
   PromptWave<T, D> p;
   auto& w = p.w;
   p.begin(a.scale, lds_own);
@@ -332,14 +333,14 @@ __global__ __launch_bounds__(64 * ROW_WAVES * PARTS, D <= 128 ? 2 : 1) void prom
   const int32_t all = wave_here > 0 ? (int32_t)((first + 32 * row_wave) / a.G) + 1 : 0;
   const int32_t most = wave_here > 0 ? (int32_t)((first + 32 * row_wave + (wave_here < 32 ? wave_here : 32) - 1) / a.G) + 1 : 0;
   const int32_t end = (int32_t)((first + here - 1) / a.G) + 1;
-  const int32_t tiles = (end + kPromptTile - 1) / kPromptTile, steps = (tiles + PARTS - 1) / PARTS;
+  const int32_t tiles = (end + kPromptTile - 1) / kPromptTile;
 
   const One* const keys = static_cast<const One*>(a.k.data) + seq.from * a.k.token_stride + head * a.k.head_stride;
   const One* const values = static_cast<const One*>(a.v.data) + seq.from * a.v.token_stride + head * a.v.head_stride;
   typedef TileLoads<R, WAVES> Loads;
   const Loads of_keys(a.k.token_stride, wave, lane), of_values(a.v.token_stride, wave, lane);
   // (the wave has read what lies in the stage: it waits for its reads before the barrier that all loads stand behind)
-  const auto load_tile = [&](int32_t tile, uint32_t to) {
+  const auto load = [&](int32_t tile, uint32_t to) {
     const int32_t left = seq.length - tile * kPromptTile;
     const One* const k = keys + (int64_t)tile * kPromptTile * a.k.token_stride;
     const One* const v = values + (int64_t)tile * kPromptTile * a.v.token_stride;
@@ -351,36 +352,31 @@ __global__ __launch_bounds__(64 * ROW_WAVES * PARTS, D <= 128 ? 2 : 1) void prom
       Loads::fetch_part(lds + to + 2 * R::kHalf, v, a.v.token_stride, left, wave, lane);
     }
   };
-  const auto load = [&](int32_t step, uint32_t to) {
-#pragma unroll
-    for (int x = 0; x < PARTS; ++x)
-      if (x == 0 || step * PARTS + x < tiles) load_tile(step * PARTS + x, to + x * kTileBytes);
-  };
   load(0, 0);
   queries();
   __builtin_amdgcn_s_waitcnt(0x0f70);                    // vmcnt(0), with the builtin, so that the compiler knows and does not wait for the queries in the loop
   const auto next = [&](int32_t j, uint32_t at) {
     wait_loads<0>();
     meet();                                              // the tile is there, and all are done with the one before
-    if (j + 1 < steps) load(j + 1, at ^ kStage);
+    if (j + 1 < tiles) load(j + 1, at ^ kStage);
   };
-  const int32_t whole = (all / kPromptTile - part + PARTS - 1) / PARTS;    // steps (all / kPromptTile: at most tiles)
+  const int32_t whole = (all / kOwn - part + PARTS - 1) / PARTS;           // tiles of which the wave's rows see all of its part
   int32_t j = 0;
   for (; j + 2 <= whole; j += 2) {
     next(j, 0);
-    p.whole(0);
+    p.template whole<BLOCKS>(0);
     next(j + 1, kStage);
-    p.whole(kStage);
+    p.template whole<BLOCKS>(kStage);
   }
   if (j < whole) {
     next(j++, 0);
-    p.whole(0);
+    p.template whole<BLOCKS>(0);
   }
-  for (; j < steps; ++j) {
+  for (; j < tiles; ++j) {
     const uint32_t at = j % 2 * kStage;
     next(j, at);
-    const int32_t from = (j * PARTS + part) * kPromptTile;
-    if (most > from) p.edge(lds_own, at, sees - from, most - from);
+    const int32_t from = (j * PARTS + part) * kOwn;
+    if (most > from) p.edge(lds_own, at, sees - from < kOwn ? sees - from : kOwn, most - from < kOwn ? most - from : kOwn);
   }
 
   if constexpr (PARTS == 2) {
@@ -409,8 +405,9 @@ __global__ __launch_bounds__(64 * ROW_WAVES * PARTS, D <= 128 ? 2 : 1) void prom
 template <class T, int D, int ROW_WAVES, int PARTS>
 void prompt_as(PromptArgs a, hipStream_t st) {
   a.tiles = (int32_t)((int64_t)a.tokens * a.G / (32 * ROW_WAVES) + a.sequences);
-  prompt_kernel<T, D, ROW_WAVES, PARTS><<<(uint32_t)a.tiles * (uint32_t)a.Hk, 64 * ROW_WAVES * PARTS, kPromptStages * PARTS * PromptWave<T, D>::kStage, st>>>(a);
+  prompt_kernel<T, D, ROW_WAVES, PARTS><<<(uint32_t)a.tiles * (uint32_t)a.Hk, 64 * ROW_WAVES * PARTS, kPromptStages * PromptWave<T, D>::kStage, st>>>(a);
 }
+
 // The workgroup of a launch, by the items (tiles of rows, kv heads) that it has at most.
 //
 // Eight waves of rows share what four would load each: worth it where there are two such workgroups a CU at least and sequences are long beside a
@@ -418,25 +415,19 @@ void prompt_as(PromptArgs a, hipStream_t st) {
 // part is wasted and the longest item is longer: 16 sequences of 1 .. 1024 tokens 92 and 83, one of 2048 55 and 48.  Heads of 64 and 96
 // load little (4 x 8192 of 16 of 64 672 and 629, 8192 of 32 on 8 of 96 471 and 470), those of 256 have no room.
 //
-// Where four waves of rows leave CUs without work, or with one wave a SIMD, two waves share each row's tokens: the time is that of the longest run
-// of tiles.  Tiles of 64 rows, while there is about one a CU (heads of 64: two, which LDS has room for); us, with four waves of 128
-// rows: 2048 tokens of 8 heads of 64 18.0 (27.8), 16 19.8 (28.1), 24 25.7 (28.7), 4 x 512 of 16 10.6 (12.9), 20 14.1 (13.7); of 8 heads of 128 27.1
-// (38.8), 4 x 512 of 8 11.9 (15.2), 12 20.2 (15.9).  Then tiles of 128 rows: 2048 tokens of 16 heads of 128 33.8 (39.6), 24 38.7 (43.2),
-// 4 x 512 of 16 16.1 (17.9), 20 25.6 (20.7).  (Sequences of 70 tokens: 7.2 for 6.9; of 100: 7.3 for 7.9.)
+// Where four waves of rows leave CUs without work, or with one wave a SIMD, two waves of rows have tiles of 64, and two waves share each row's
+// tokens: the time is that of the longest run of tiles.  us, with four waves of rows in brackets: 2048 tokens of 8 heads of 64 20.2 (28.1), 24 23.1 (28.6),
+// 32 29.0 (29.9); of 8 heads of 128 28.5 (39.3), 24 38.0 (43.3), 32 47.8 (47.6); 4 x 512 of 16 15.3 (18.0), 24 23.2 (22.4), 32 25.3 (21.9).  Sequences of
+// 70 tokens 7.2 (6.9), of 100 7.3 (7.9).  Heads of 256 spill: 2048 tokens of 8 117 (78).  (Both waves with whole tiles, of 128 tokens
+// a step, which leaves heads of 128 one workgroup a CU: 2048 tokens of 8 heads 27.1, 16 33.6 for 31.5, 24 52.8.)
 template <class T, int D>
 void prompt_of(const PromptArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.tokens * a.G;
-  const auto items = [&](int64_t wide) { return (rows / wide + a.sequences) * a.Hk; };
   if constexpr (D == 128) {
     if (rows >= 4096 * (int64_t)a.sequences && rows / 256 * a.Hk >= 512) return prompt_as<T, D, 8, 1>(a, st);
   }
   if constexpr (D <= 128) {
-    if (2 * (int64_t)a.tokens >= 3 * kPromptTile * (int64_t)a.sequences) {
-      if (items(64) <= (D == 64 ? 640 : 320)) return prompt_as<T, D, 2, 2>(a, st);
-      if constexpr (D > 64) {
-        if (items(128) <= 336) return prompt_as<T, D, 4, 2>(a, st);
-      }
-    }
+    if (2 * (int64_t)a.tokens >= 3 * kPromptTile * (int64_t)a.sequences && (rows / 64 + a.sequences) * a.Hk <= 960) return prompt_as<T, D, 2, 2>(a, st);
   }
   prompt_as<T, D, 4, 1>(a, st);
 }
