@@ -12,7 +12,7 @@
 // LDS, 32 rows a wave, take about as long as the products.  64 rows a wave, half of these reads, leave one wave a SIMD: its accumulators move
 // between register files, 1.78 us a tile of 256 rows for 1.5, and 25 us before and behind.  Short ones are bound by what comes one after the
 // other: 0.75 .. 0.95 us a tile of 64 tokens for a wave, 6.5 us of launch, first loads and results.  5 sequences of 331 .. 777 tokens, 12 heads of 64:
-// 13.1 us; 16 of 1 .. 1024, 32 on 8 of 128: 75 .. 81 (35 at the rate of a large product).
+// 12.2 us; 16 of 1 .. 1024, 32 on 8 of 128: 75 .. 82 (35 at the rate of a large product).
 //
 // Scores of the next tile before the softmax of one, which would keep the matrix cores busy with one wave, spill; with two waves a SIMD the other
 // does that.  Four tiles in LDS instead of two leave one workgroup a CU, and gained nothing.

@@ -294,7 +294,7 @@ def test_launches_that_fill_the_chip(gen, lengths, H, Hk, D, dtype):
 
 
 # kv heads and heads of each that take sequences of 200 and 60 tokens through every kind of workgroup
-FORMS = [(2, 4), (64, 1), (128, 1), (16, 32)]
+FORMS = [(2, 4), (128, 1), (192, 1), (16, 32)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F16])
