@@ -27,6 +27,7 @@ struct PromptArgs {
   csd_heads q, k, v;
   const int32_t* offsets;
   int32_t sequences, tokens, Hk, G, tiles;
+  bool turned;                           // tiles of a sequence are few: see turned_about()
   float scale;                           // times log2(e)
   void* out;
   float* lse;
@@ -291,6 +292,15 @@ struct PromptWave {
   }
 };
 
+// Workgroups go round the 8 XCDs and an XCD's round its 4 shader engines, whatever these have to do: where every second or fourth tile is empty, as
+// with sequences of one or three tiles, one or two engines of four get nothing.  So each turn of 32 begins at another engine.  (512 sequences of 32
+// tokens, 32 heads of 128 on 8, 89 us for 157, 170 of 96 90 for 117; 256 of 64, whose tiles go round evenly, 94 for 89; longer ones, that
+// have few empty tiles, lose 1 .. 4 %.)
+__device__ inline uint32_t turned_about(uint32_t block, uint32_t blocks) {
+  const uint32_t turn = block / 32, of = block / 8 + turn + turn / 4;
+  return (block | 31) < blocks ? turn * 32 + of % 4 * 8 + block % 8 : block;
+}
+
 // PARTS waves share a row, BLOCKS blocks of a tile's two each, and add up what they have at the end.
 template <class T, int D, int ROW_WAVES, int PARTS>
 __global__ __launch_bounds__(64 * ROW_WAVES * PARTS, D <= 128 ? 2 : 1) void prompt_kernel(PromptArgs a) {
@@ -303,8 +313,9 @@ __global__ __launch_bounds__(64 * ROW_WAVES * PARTS, D <= 128 ? 2 : 1) void prom
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row_wave = wave % ROW_WAVES, part = wave / ROW_WAVES;
   // A sequence's last tiles, the longest runs of tokens, go first.  (Sequences in order of their lengths too, the longest ones first: 16 of 32 .. 1024
   // tokens 76 us for 78, 16 of 256 30 for 28, one of 4096 before or behind seven of 1000 214 for 208 and 213 for 212.)
-  const int32_t head = blockIdx.x % (uint32_t)a.Hk;
-  const Sequence seq = sequence_of(a.offsets, a.sequences, a.tokens, a.tiles - 1 - blockIdx.x / (uint32_t)a.Hk, kPromptRows, a.G);
+  const uint32_t item = a.turned ? turned_about(blockIdx.x, gridDim.x) : blockIdx.x;
+  const int32_t head = item % (uint32_t)a.Hk;
+  const Sequence seq = sequence_of(a.offsets, a.sequences, a.tokens, a.tiles - 1 - item / (uint32_t)a.Hk, kPromptRows, a.G);
   const int64_t rows = (int64_t)seq.length * a.G, first = (int64_t)seq.tile * kPromptRows;
   if (first >= rows) return;
   const int32_t here = rows - first < kPromptRows ? (int32_t)(rows - first) : kPromptRows;
@@ -405,6 +416,7 @@ __global__ __launch_bounds__(64 * ROW_WAVES * PARTS, D <= 128 ? 2 : 1) void prom
 template <class T, int D, int ROW_WAVES, int PARTS>
 void prompt_as(PromptArgs a, hipStream_t st) {
   a.tiles = (int32_t)((int64_t)a.tokens * a.G / (32 * ROW_WAVES) + a.sequences);
+  a.turned = (int64_t)a.tokens * a.G <= 3 * 32 * ROW_WAVES * (int64_t)a.sequences;
   prompt_kernel<T, D, ROW_WAVES, PARTS><<<(uint32_t)a.tiles * (uint32_t)a.Hk, 64 * ROW_WAVES * PARTS, kPromptStages * PromptWave<T, D>::kStage, st>>>(a);
 }
 

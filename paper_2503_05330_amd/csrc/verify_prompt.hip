@@ -22,7 +22,7 @@ extern "C" int csd_prompt_attend(const csd_heads* q, const csd_heads* k, const c
   const int64_t tiles = tokens * G / 128 + sequences;
   if (tiles * n_kv_heads > 1 << 23) return CSD_ERR_INVALID_ARG;
   if (tokens == 0) return CSD_OK;
-  const PromptArgs a{*q, *k, *v, d_offsets, sequences, (int32_t)tokens, n_kv_heads, G, (int32_t)tiles, scale * kLog2E, d_out, d_lse};
+  const PromptArgs a{*q, *k, *v, d_offsets, sequences, (int32_t)tokens, n_kv_heads, G, (int32_t)tiles, false, scale * kLog2E, d_out, d_lse};
   hipStream_t st = static_cast<hipStream_t>(stream);
   switch (head_dim) {
     case 64: prompt_64(a, type == CSD_F16, st); break;

@@ -331,3 +331,9 @@ def test_every_workgroup_with_tokens_that_weigh_nothing(gen, Hk, G, D):
         assert ((out[a:b].double() - want).abs() <= error * (1 + 2.0 ** -7)).all()
         assert ((lse[a:b].double() - n.log()[:, None]).abs()[n > 0] <= 2.0 ** -20 * 6).all() and (lse[a:b][n == 0] == -torch.inf).all()
     assert not out[:70].any()
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("lengths,G", [([32] * 40, 4), ([96] * 25, 4), ([5] * 33, 1), ([64, 1, 33] * 21, 3)])
+def test_many_sequences_of_few_tiles(gen, lengths, G, D):
+    check(gen, lengths, 8 * G, 8, D)
