@@ -2,8 +2,9 @@
 //
 // A workgroup has eight tokens: their pairs' turns are worked out once, in LDS, and serve all heads.  What bounds it: memory.  8 x 4096 tokens of 40
 // heads of 128: 131 us, 5.1 TB/s, what a copy reaches; sixteen tokens 4.3 us, launch and round trips.  With the write, 64 x 16 x 9
-// tokens of 32 + 8 + 8 heads, to 8 bits: 40 .. 47 us, 3.8 .. 4.5 TB/s.  One launch instead of two saves keys a write and a read, and
-// the launch.  (Asking for the next job's values before one is turned: 45 us for 42; six waves a SIMD, by spilling: 69; banks'
+// tokens of 32 + 8 + 8 heads, to 8 bits: 42 us of 66 with their reading, 4.3 TB/s.  One launch instead of two saves keys a write and a read, and
+// the launch.  Of queries a thread holds both eights of eight pairs (as keys are, an eight at a time with its pairs' others read beside: 69.5; queries
+// before keys: 67.4).  (Asking for the next values before one is turned: 3 us more; six waves a SIMD, by spilling: 30 more; banks'
 // conflicts of the turns' reads taken away, sines of a shorter series, workgroups of half the heads: the same.)
 #include <cmath>
 
@@ -24,56 +25,46 @@ struct RotateArgs {
   int32_t heads, dim, per;               // per: heads of a workgroup
 };
 
-// Eight tokens of `per` heads; a thread takes sixteen values of a token's head at a time, both eights of eight pairs (or, behind them, two
-// eights to be copied): two reads and two writes of 16 bytes, which the threads of a head and of the next ones do side by side.
-template <class T>
-__global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs a) {
+// Rotates heads head0 .. head0 + heads - 1 of `here` tokens.  A thread takes sixteen values of a token's head at a time, both eights of eight pairs
+// (or, behind them, two eights to be copied): two reads and two writes of 16 bytes, which the threads of a head and of the next ones do
+// side by side.  from(token), to(token): where a token's heads lie.
+template <class T, class From, class To>
+__device__ inline void rotate_heads(const csd_rotary& how, Turn* turns, int32_t here, int32_t head0, int32_t heads, int32_t dim, int64_t from_head, int64_t to_head,
+                                    From from, To to) {
   typedef typename T::Eight Eight;
   typedef typename T::One Value;
-  extern __shared__ Turn turns[];
-  const int64_t first = (int64_t)blockIdx.x * kGroup;
-  const int32_t here = a.tokens - first < kGroup ? (int32_t)(a.tokens - first) : kGroup;
-  const int32_t pairs = a.how.dim / 2;
-  for (int32_t x = threadIdx.x; x < here * pairs; x += kRotateThreads) {
-    const int32_t token = x / pairs;
-    Turns(turns, token, pairs)[x - token * pairs] = turn_of(a.how, a.positions[first + token], x - token * pairs);
-  }
-  __syncthreads();
-  const int32_t head0 = blockIdx.y * a.per, heads = a.heads - head0 < a.per ? a.heads - head0 : a.per;
-  const int32_t turning = a.how.dim / 16, units = turning + (a.dim - a.how.dim + 15) / 16, all = here * heads * units;
+  const int32_t pairs = how.dim / 2, turning = how.dim / 16, units = turning + (dim - how.dim + 15) / 16, all = here * heads * units;
   constexpr int kAhead = 2;                              // (4: 133 us for 131 with 8 x 4096 tokens of 40 heads of 128; a copy of as much takes 130)
   for (int32_t x0 = threadIdx.x; x0 < all; x0 += kAhead * kRotateThreads) {
     Eight u[kAhead], v[kAhead];
-    int64_t to[kAhead];
-    int32_t d[kAhead], e[kAhead], token[kAhead];         // where the two eights lie; e < 0: there is no second
+    int32_t d[kAhead], e[kAhead], token[kAhead], head[kAhead];           // where the two eights lie; e < 0: there is no second
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
       const int32_t x = x0 + s * kRotateThreads < all ? x0 + s * kRotateThreads : x0;
       const int32_t row = x / units, unit = x - row * units;
       token[s] = row / heads;
-      const int32_t head = head0 + row - token[s] * heads;
+      head[s] = head0 + row - token[s] * heads;
       if (unit < turning) {
-        d[s] = a.how.interleaved ? 16 * unit : 8 * unit;
-        e[s] = a.how.interleaved ? d[s] + 8 : d[s] + pairs;
+        d[s] = how.interleaved ? 16 * unit : 8 * unit;
+        e[s] = how.interleaved ? d[s] + 8 : d[s] + pairs;
       } else {
-        d[s] = a.how.dim + 16 * (unit - turning);
-        e[s] = d[s] + 8 < a.dim ? d[s] + 8 : -1;
+        d[s] = how.dim + 16 * (unit - turning);
+        e[s] = d[s] + 8 < dim ? d[s] + 8 : -1;
       }
-      const Value* const from = static_cast<const Value*>(a.x.data) + (first + token[s]) * a.x.token_stride + head * a.x.head_stride;
-      to[s] = (first + token[s]) * a.out.token_stride + head * a.out.head_stride;
-      u[s] = *reinterpret_cast<const Eight*>(from + d[s]);
-      v[s] = *reinterpret_cast<const Eight*>(from + (e[s] < 0 ? d[s] : e[s]));
+      const Value* const x_of = from(token[s]) + head[s] * from_head;
+      u[s] = *reinterpret_cast<const Eight*>(x_of + d[s]);
+      v[s] = *reinterpret_cast<const Eight*>(x_of + (e[s] < 0 ? d[s] : e[s]));
     }
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
       if (x0 + s * kRotateThreads >= all) break;
-      Value* const out = static_cast<Value*>(const_cast<void*>(a.out.data)) + to[s];
+      Value* const out = to(token[s]) + head[s] * to_head;
       Eight y = u[s], z = v[s];
-      if (d[s] < a.how.dim) {
+      if (d[s] < how.dim) {
         const Turns own(turns, token[s], pairs);
-        if (a.how.interleaved) {
-          y = turned_eight<T>(u[s], v[s], d[s], a.how, own);
-          z = turned_eight<T>(v[s], u[s], e[s], a.how, own);
+        if (how.interleaved) {
+          y = turned_eight<T>(u[s], v[s], d[s], how, own);
+          z = turned_eight<T>(v[s], u[s], e[s], how, own);
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {                  // a pair's turn, read once for both
@@ -89,6 +80,31 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs a) {
   }
 }
 
+// the turns of a workgroup's tokens
+__device__ inline void make_turns(const csd_rotary& how, const int32_t* positions, int32_t here, Turn* turns) {
+  const int32_t pairs = how.dim / 2;
+  for (int32_t x = threadIdx.x; x < here * pairs; x += kRotateThreads) {
+    const int32_t token = x / pairs;
+    Turns(turns, token, pairs)[x - token * pairs] = turn_of(how, positions[token], x - token * pairs);
+  }
+}
+
+// eight tokens, `per` heads
+template <class T>
+__global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs a) {
+  typedef typename T::One Value;
+  extern __shared__ Turn turns[];
+  const int64_t first = (int64_t)blockIdx.x * kGroup;
+  const int32_t here = a.tokens - first < kGroup ? (int32_t)(a.tokens - first) : kGroup;
+  make_turns(a.how, a.positions + first, here, turns);
+  __syncthreads();
+  const int32_t head0 = blockIdx.y * a.per, heads = a.heads - head0 < a.per ? a.heads - head0 : a.per;
+  const Value* const x = static_cast<const Value*>(a.x.data) + first * a.x.token_stride;
+  Value* const out = static_cast<Value*>(const_cast<void*>(a.out.data)) + first * a.out.token_stride;
+  rotate_heads<T>(a.how, turns, here, head0, heads, a.dim, a.x.head_stride, a.out.head_stride,
+                  [&](int32_t token) { return x + token * a.x.token_stride; }, [&](int32_t token) { return out + token * a.out.token_stride; });
+}
+
 struct PlaceArgs {
   csd_rotary how;
   csd_heads q;
@@ -99,13 +115,14 @@ struct PlaceArgs {
   int32_t H, per;                        // per: jobs of a workgroup.  A job: a kv head's keys and values, or a query head
 };
 
-// Eight tokens, of one path or of several; a wave takes a job of theirs at a time, eight lanes a token.
+// Eight tokens, of one path or of several.  Keys and values: a wave takes a kv head's at a time, eight lanes a token; then queries, as rotate_kernel().
 template <class T, int D, bool FP8>
 __global__ __launch_bounds__(kRotateThreads) void place_kernel(PlaceArgs a) {
   typedef typename T::Eight Eight;
   typedef typename T::One Value;
   typedef Pieces<D> P;
   __shared__ Turn turns[Turns::size(kGroup, D / 2)];
+  __shared__ int64_t queries[kGroup];                    // where the tokens' begin
   const int wave = threadIdx.x >> 6, nth = (threadIdx.x & 63) / 8;
   const int64_t first = (int64_t)blockIdx.x * kGroup;
   const int32_t here = a.tokens - first < kGroup ? (int32_t)(a.tokens - first) : kGroup;
@@ -118,52 +135,34 @@ __global__ __launch_bounds__(kRotateThreads) void place_kernel(PlaceArgs a) {
   count = count > m.n ? m.n : count;
   const int64_t pos = (int64_t)(m.start ? m.start[row] : 0) + t;
   const bool asked = there && t < count, live = asked && pos >= 0 && pos < m.held.cap;
-  for (int32_t x = threadIdx.x; x < here * pairs; x += kRotateThreads) {
-    const int32_t of = x / pairs;
-    Turns(turns, of, pairs)[x - of * pairs] = turn_of(a.how, a.positions[first + of], x - of * pairs);
-  }
+  if (wave == 0 && (threadIdx.x & 7) == 0) queries[nth] = row * a.q.row_stride + t * a.q.token_stride;
+  make_turns(a.how, a.positions + first, here, turns);
   if (wave == 0 && blockIdx.y == 0 && asked && !live) atomicOr(m.status, CSD_STATUS_CAPACITY);
   __syncthreads();
-  const auto load = [&](const Value* from, Eight (&x)[P::kPieces], bool wanted) {
-#pragma unroll
-    for (int i = 0; i < P::kPieces; ++i) {
-      x[i] = Eight{};
-      if (wanted && P::d(i) < D) x[i] = *reinterpret_cast<const Eight*>(from + P::d(i));
-    }
-  };
-  const auto rotate = [&](const Value* from, Eight (&x)[P::kPieces], bool wanted) {
-    Eight other[P::kPieces];
+  const int32_t job0 = blockIdx.y * a.per, end = job0 + a.per < m.Hk + a.H ? job0 + a.per : m.Hk + a.H;
+  for (int32_t head = job0 + wave; head < end && head < m.Hk; head += kMoveWaves) {
+    const Value* const k_from = static_cast<const Value*>(m.k.data) + row * m.k.row_stride + t * m.k.token_stride + head * m.k.head_stride;
+    const Value* const v_from = static_cast<const Value*>(m.v.data) + row * m.v.row_stride + t * m.v.token_stride + head * m.v.head_stride;
+    Eight k[P::kPieces], v[P::kPieces], other[P::kPieces];
 #pragma unroll
     for (int i = 0; i < P::kPieces; ++i) {
       const int d = P::d(i), e = d < pairs ? d + pairs : d - pairs;
-      other[i] = Eight{};
-      if (wanted && d < a.how.dim && !a.how.interleaved) other[i] = *reinterpret_cast<const Eight*>(from + e);
+      k[i] = v[i] = other[i] = Eight{};
+      if (live && d < D) {
+        k[i] = *reinterpret_cast<const Eight*>(k_from + d);
+        v[i] = *reinterpret_cast<const Eight*>(v_from + d);
+        if (d < a.how.dim && !a.how.interleaved) other[i] = *reinterpret_cast<const Eight*>(k_from + e);
+      }
     }
 #pragma unroll
     for (int i = 0; i < P::kPieces; ++i)
-      if (wanted && P::d(i) < a.how.dim) x[i] = turned_eight<T>(x[i], other[i], P::d(i), a.how, Turns(turns, nth, pairs));
-  };
-  const int32_t job0 = blockIdx.y * a.per, end = job0 + a.per < m.Hk + a.H ? job0 + a.per : m.Hk + a.H;
-  for (int32_t job = job0 + wave; job < end; job += kMoveWaves) {
-    Eight x[P::kPieces];
-    if (job < m.Hk) {
-      Eight v[P::kPieces];
-      const Value* const k_from = static_cast<const Value*>(m.k.data) + row * m.k.row_stride + t * m.k.token_stride + job * m.k.head_stride;
-      load(k_from, x, live);
-      load(static_cast<const Value*>(m.v.data) + row * m.v.row_stride + t * m.v.token_stride + job * m.v.head_stride, v, live);
-      rotate(k_from, x, live);
-      hold<T, D, FP8>(m.held, m.held.first(row, job, m.Hk) + (live ? pos / kBlock : 0), (int)pos & (kBlock - 1), live, x, v);
-    } else {
-      const int32_t head = job - m.Hk;
-      const Value* const from = static_cast<const Value*>(a.q.data) + row * a.q.row_stride + t * a.q.token_stride + head * a.q.head_stride;
-      load(from, x, there);
-      rotate(from, x, there);
-      if (!there) continue;
-#pragma unroll
-      for (int i = 0; i < P::kPieces; ++i)
-        if (P::d(i) < D) *reinterpret_cast<Eight*>(static_cast<Value*>(a.q_out) + (token * a.H + head) * D + P::d(i)) = x[i];
-    }
+      if (live && P::d(i) < a.how.dim) k[i] = turned_eight<T>(k[i], other[i], P::d(i), a.how, Turns(turns, nth, pairs));
+    hold<T, D, FP8>(m.held, m.held.first(row, head, m.Hk) + (live ? pos / kBlock : 0), (int)pos & (kBlock - 1), live, k, v);
   }
+  const int32_t head0 = job0 < m.Hk ? 0 : job0 - m.Hk, heads = end - m.Hk - head0;
+  if (heads > 0)
+    rotate_heads<T>(a.how, turns, here, head0, heads, D, a.q.head_stride, D, [&](int32_t x) { return static_cast<const Value*>(a.q.data) + queries[x]; },
+                    [&](int32_t x) { return static_cast<Value*>(a.q_out) + (first + x) * a.H * D; });
 }
 
 // Workgroups share a group's heads where there are few groups: until there are so many workgroups, or each wave has one.  (1024 and 2048: the
