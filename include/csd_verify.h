@@ -201,6 +201,7 @@ int csd_cache_write_packed(csd_cache* cache, int32_t layer, const csd_heads* k, 
  *   q, k, v  tokens of n_heads, n_kv_heads, n_kv_heads heads (row_stride is not used); n_heads is a multiple of n_kv_heads, up to CSD_MAX_HEADS
  *   d_out    [tokens][n_heads][head_dim] dense, 16-byte aligned = sum_x softmax_x(scale * q.k_x) v_x, must not overlap q, k, v
  *   d_lse    [tokens][n_heads] float = ln sum_x exp(scale * q.k_x), may be NULL
+ * The same call gives the same bits; how a token's sums are ordered may depend on what else is packed.
  * Tokens of no sequence are not written.  Nothing that a token does not see, not even an infinity or a NaN, changes its result; where
  * all that it sees weighs nothing (every score -inf), it gets zeros and -inf.
  * head_dim 64, 96, 128 or 256 (else CSD_ERR_UNIMPLEMENTED), type CSD_BF16 or CSD_F16; scale finite, times log2 e too; token strides of k and v

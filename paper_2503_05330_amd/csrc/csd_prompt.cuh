@@ -4,7 +4,8 @@
 // token, rows of a sequence lie behind each other (row = token * G + g), and a workgroup takes a tile of them for a kv head: what it
 // loads of keys and values serves all G heads.  A wave has 32 rows, in the orientation of csd_attend.cuh: S^T = K Q^T and O^T += V^T P^T
 // with a running (near) maximum and sum, no weight leaving its lane.  Keys and values come in tiles of 64 tokens to a ring of two in
-// LDS, by loads that pass no register, the next tile's during the products of one; all waves of the workgroup read the same.
+// LDS, by loads that pass no register, the next tile's during the products of one; all waves of the workgroup read the same (or,
+// where two share a row, a block each).
 // Tiles that all rows see whole come first, without a mask; the last few, of which rows see a part, are edge()'s.
 //
 // What bounds it: at length power, then LDS.  One sequence of 16384 tokens, 28 heads of 128 on 4: 1.66 .. 1.74 ms, 1100 .. 1160 TFLOP/s (a product
