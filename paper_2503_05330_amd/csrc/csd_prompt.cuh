@@ -41,28 +41,37 @@ constexpr int kPromptTile = 2 * kBlock, kPromptStages = 2;
 template <class R, int WAVES>
 struct TileLoads {
   static constexpr int kAll = 2 * R::kPieces, kPieces = (kAll + WAVES - 1) / WAVES;              // piece wave + WAVES x, where it is one of all
-  static constexpr int kApart = 64 * WAVES / R::kChunks;                                         // tokens from one to the next
+  static constexpr int kApart = 64 * WAVES / R::kChunks;                                         // tokens from one to the next, where chunks are a power of two
   static __device__ bool there(int x, int wave) { return kAll % WAVES == 0 || wave + WAVES * x < kAll; }
-  static constexpr bool kAlike = R::kSwizzled;           // the lane's places in its pieces differ by whole tokens and a constant order of chunks
-  uint32_t at[kAlike ? 1 : kPieces];
-  static __device__ uint32_t place(int x, int64_t stride, int32_t left, int wave, int lane) {
+  // The lane's places in pieces x and x + kOrders lie whole tokens apart, which a wave's address takes: their chunks are in the same order.  (The order is
+  // part of the place: a turn put on a sum of tokens and chunks also meets bits of the tokens' where strides are no multiples of 32.)
+  static constexpr int orders() {
+    if (!R::kSwizzled) return kPieces;
+    for (int n = 1; n < kPieces; ++n) {
+      bool again = true;
+      for (int x = n; x < kPieces; ++x) again = again && R::swizzle(x * kApart & 31) == R::swizzle(x % n * kApart & 31);
+      if (again) return n;
+    }
+    return kPieces;
+  }
+  static constexpr int kOrders = orders();               // heads of 64, 128: 1; of 256: 2
+  uint32_t at[kOrders];
+  static __host__ __device__ uint32_t place(int x, int64_t stride, int32_t left, int wave, int lane) {
     const int chunk = (wave + WAVES * x) * 64 + lane, row = chunk / R::kChunks, token = row < left ? row : left - 1;
     return (uint32_t)token * (uint32_t)stride * 2 + (uint32_t)(chunk % R::kChunks ^ R::swizzle(row & 31)) * 16;
   }
-  __device__ TileLoads(int64_t stride, int wave, int lane) {
+  __host__ __device__ TileLoads(int64_t stride, int wave, int lane) {
 #pragma unroll
-    for (int x = 0; x < (kAlike ? 1 : kPieces); ++x) at[x] = place(x, stride, kPromptTile, wave, lane);
+    for (int x = 0; x < kOrders; ++x) at[x] = place(x, stride, kPromptTile, wave, lane);
   }
-  // a tile whose tokens are all there
+  // A tile whose tokens are all there: the lane's 16 bytes of piece x lie at `lane_at(x)` bytes behind element `wave_at(x)` of its own.
+  static __host__ __device__ int64_t wave_at(int x, int64_t stride) { return (int64_t)(x - x % kOrders) * kApart * stride; }
+  __host__ __device__ uint32_t lane_at(int x) const { return at[x % kOrders]; }
   template <class One>
   __device__ void fetch_to(uint32_t lds, const One* from, int64_t stride, int wave) const {
 #pragma unroll
-    for (int x = 0; x < kPieces; ++x) {
-      if (!there(x, wave)) continue;
-      const uint32_t to = uniform(lds + 1024u * (WAVES * x + wave));
-      if constexpr (kAlike) fetch(to, uniform(reinterpret_cast<const uint8_t*>(from + x * kApart * stride)), at[0] ^ R::swizzle(x * kApart & 31) << 4);
-      else fetch(to, uniform(reinterpret_cast<const uint8_t*>(from)), at[x]);
-    }
+    for (int x = 0; x < kPieces; ++x)
+      if (there(x, wave)) fetch(uniform(lds + 1024u * (WAVES * x + wave)), uniform(reinterpret_cast<const uint8_t*>(from + wave_at(x, stride))), lane_at(x));
   }
   template <class One>
   static __device__ void fetch_part(uint32_t lds, const One* from, int64_t stride, int32_t left, int wave, int lane) {
