@@ -567,7 +567,9 @@ PyObject* cache_write_rotated(PyObject*, PyObject* const* args, Py_ssize_t n_arg
   for (int i = 0; i < 3; ++i)
     if (c.at + i < c.n && THPVariable_CheckExact(c.args[c.at + i])) d.holds(c, &THPVariable_Unpack(c.args[c.at + i]));
   const csd_heads q = heads_of(c, x, x.N, x.H, &n), k = heads_of(c, x, x.N, x.Hk, &n), v = heads_of(c, x, x.N, x.Hk, &n);
-  const int64_t rows = x.P * x.N;
+  const int64_t rows = x.P * x.N, of_positions[] = {x.P, x.N, n};
+  const at::Tensor* positions = peek(c, 3);
+  if (!positions || positions->sizes() != c10::IntArrayRef(of_positions, 3)) c.usual = false;
   const int32_t* at = ints_of(c, d, rows * n, false);
   const int32_t *start = ints_of(c, d, rows, true), *counts = ints_of(c, d, rows, true);
   if (!c.usual) Py_RETURN_NONE;

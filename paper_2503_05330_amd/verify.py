@@ -245,6 +245,8 @@ class PathCache:
         _here(q, k, v, positions, start, counts)
         if v.shape != k.shape or k.shape[-3] != n:
             raise ValueError("queries of shape %s, keys of %s, values of %s" % (tuple(q.shape), tuple(k.shape), tuple(v.shape)))
+        if positions.shape != (*lead, n):
+            raise ValueError("positions of shape %s, needs %s" % (tuple(positions.shape), (*lead, n)))
         out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
         _check(load().csd_cache_write_rotated(self._h, layer, rotary._config(), ctypes.byref(qh), ctypes.byref(kh), ctypes.byref(vh),
                                               _ptr(positions, torch.int32, rows * n), _ptr(start, torch.int32, rows),

@@ -1,0 +1,32 @@
+"""Tensors of other shapes than the operators around the cache take: with numbers enough, they were read as if they were of the right one."""
+import pytest
+import torch
+
+from paper_2503_05330_amd import verify
+from test_around_calls import Declines
+from test_verify import BF, gen, ints, normal, same  # noqa: F401 (gen: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(params=["native", "python"])
+def way(request, monkeypatch):
+    """Both ways that a call is marshalled."""
+    verify.load()
+    if request.param == "python":
+        monkeypatch.setattr(verify, "_native", Declines())
+
+
+def test_positions_of_another_shape_are_refused(gen, way):
+    P, N, n, H, Hk, D = 2, 3, 4, 4, 2, 64
+    c, rotary = verify.PathCache(P, N, 0, 16, H, Hk, D, 8), verify.Rotary(D)
+    q, k, v = normal(gen, (P, N, n, H, D), BF), normal(gen, (P, N, n, Hk, D), BF), normal(gen, (P, N, n, Hk, D), BF)
+    zero = torch.zeros((P, N, 16, Hk, D), dtype=BF, device="cuda")
+    c.write(0, zero, zero)
+    at = torch.arange(P * N * 8, dtype=torch.int32, device="cuda")
+    for wrong in (at.view(P, N, 8), at.view(N, P, 8), at[:24].view(N, P, n), at[:24].view(P, n, N), at[:24], at[:24].view(P * N, n), at[:24].view(1, P, N, n)):
+        with pytest.raises(ValueError):
+            c.write_rotated(0, q, k, v, rotary, wrong)
+    assert not c.read(0, 16)[0].any()                        # nothing was enqueued
+    right = at.view(P, N, 8)[..., :n].contiguous()
+    assert same(c.write_rotated(0, q, k, v, rotary, right), verify.rotate(q, right, rotary))
