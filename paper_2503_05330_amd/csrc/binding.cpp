@@ -669,7 +669,8 @@ PyObject* adjust(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   const at::Tensor* penalties = c.any_tensor(true);
   if (penalties) {
     d.holds(c, penalties);
-    if (penalties->scalar_type() != at::kFloat || !penalties->is_contiguous() || penalties->numel() < 3 * P) c.usual = false;
+    const int64_t of_penalties[] = {P, 3};
+    if (penalties->scalar_type() != at::kFloat || !penalties->is_contiguous() || penalties->sizes() != c10::IntArrayRef(of_penalties, 2)) c.usual = false;
     a.d_penalties = static_cast<const float*>(penalties->data_ptr());
   }
   const RowsOf bias(c, d, at::kFloat, sizes.slice(0, 1), true), mask(c, d, at::kInt, sizes.slice(0, 3), true);

@@ -459,6 +459,8 @@ def adjust(logits, tokens=None, path_len=None, counts=None, prompt=None, prompt_
         raise ValueError("bias or mask too short for %d tokens" % V)
     if tokens is not None and path_len is None:
         raise ValueError("tokens need path_len")
+    if penalties is not None and penalties.shape != (P, 3):
+        raise ValueError("penalties of shape %s, needs %s" % (tuple(penalties.shape), (P, 3)))
     if tokens is not None and path_cap == 0:
         said = None
     if prompt is not None and prompt_cap == 0:

@@ -4,7 +4,7 @@ import torch
 
 from paper_2503_05330_amd import verify
 from test_around_calls import Declines
-from test_verify import BF, gen, ints, normal, same  # noqa: F401 (gen: a fixture)
+from test_verify import BF, F32, gen, ints, normal, same  # noqa: F401 (gen: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,14 @@ def test_positions_of_another_shape_are_refused(gen, way):
     assert not c.read(0, 16)[0].any()                        # nothing was enqueued
     right = at.view(P, N, 8)[..., :n].contiguous()
     assert same(c.write_rotated(0, q, k, v, rotary, right), verify.rotate(q, right, rotary))
+
+
+def test_penalties_of_another_shape_are_refused(gen, way):
+    P, N, n, V = 4, 2, 3, 100
+    logits, tokens, length = normal(gen, (P, N, n, V), F32), torch.zeros((P, N, 5), dtype=torch.int32, device="cuda"), ints([[5] * N] * P)
+    penalties = torch.tensor([[1.5, 0.5, 0.25]] * P, device="cuda")
+    for wrong in (penalties.T.contiguous(), penalties.flatten(), penalties.repeat(1, 2), penalties.repeat(2, 1), penalties[None], penalties[:, :2].contiguous()):
+        with pytest.raises(ValueError):
+            verify.adjust(logits, tokens, length, penalties=wrong)
+    got = verify.adjust(logits, tokens, length, penalties=penalties)
+    assert torch.equal(got[..., 1:], logits[..., 1:]) and not torch.equal(got, logits)
