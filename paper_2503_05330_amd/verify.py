@@ -405,6 +405,8 @@ def prompt_attend(q, k, v, offsets, scale=None, out=None, lse=None):
     _here(out, lse, offsets)
     if out is None:
         out = torch.empty((n, H, D), dtype=q.dtype, device=q.device)
+    if out.shape != q.shape or (lse is not None and lse.shape != (n, H)):
+        raise ValueError("out of shape %s, lse of %s" % (tuple(out.shape), None if lse is None else tuple(lse.shape)))
     if offsets.dim() != 1 or len(offsets) < 2:
         raise ValueError("offsets of shape %s" % (tuple(offsets.shape),))
     if any(_overlap(out, t) for t in (q, k, v)):

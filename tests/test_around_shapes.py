@@ -41,3 +41,18 @@ def test_penalties_of_another_shape_are_refused(gen, way):
             verify.adjust(logits, tokens, length, penalties=wrong)
     got = verify.adjust(logits, tokens, length, penalties=penalties)
     assert torch.equal(got[..., 1:], logits[..., 1:]) and not torch.equal(got, logits)
+
+
+def test_results_of_attention_of_another_shape_are_refused(gen):
+    T, H, Hk, D = 10, 4, 2, 64
+    q, k, v, offsets = normal(gen, (T, H, D), BF), normal(gen, (T, Hk, D), BF), normal(gen, (T, Hk, D), BF), ints([0, 3, 10])
+    out, lse = torch.zeros((T + 1, H, D), dtype=BF, device="cuda"), torch.zeros((T + 1, H), device="cuda")
+    for wrong in (out, out[:T].view(H, T, D), out[:T].view(T, H * D), out[:T].flatten()):
+        with pytest.raises(ValueError):
+            verify.prompt_attend(q, k, v, offsets, out=wrong)
+    for wrong in (lse, lse[:T].view(H, T), lse[:T].flatten(), lse[None, :T]):
+        with pytest.raises(ValueError):
+            verify.prompt_attend(q, k, v, offsets, lse=wrong)
+    assert not out.any() and not lse.any()
+    assert verify.prompt_attend(q, k, v, offsets, out=out[:T], lse=lse[:T]).data_ptr() == out.data_ptr()
+    assert same(out[:T], verify.prompt_attend(q, k, v, offsets)) and lse[:T].any(0).all()
