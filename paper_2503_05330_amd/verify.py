@@ -261,6 +261,8 @@ class PathCache:
         if v.shape != k.shape or k.dim() != 3:
             raise ValueError("keys of shape %s, values of shape %s" % (tuple(k.shape), tuple(v.shape)))
         _here(offsets)
+        if offsets.shape != (self.P + 1,):
+            raise ValueError("offsets of shape %s, needs %s" % (tuple(offsets.shape), (self.P + 1,)))
         _check(load().csd_cache_write_packed(self._h, layer, ctypes.byref(kh), ctypes.byref(vh), _ptr(offsets, torch.int32, self.P + 1),
                                              len(k), _stream()), "csd_cache_write_packed")
 

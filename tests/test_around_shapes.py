@@ -56,3 +56,17 @@ def test_results_of_attention_of_another_shape_are_refused(gen):
     assert not out.any() and not lse.any()
     assert verify.prompt_attend(q, k, v, offsets, out=out[:T], lse=lse[:T]).data_ptr() == out.data_ptr()
     assert same(out[:T], verify.prompt_attend(q, k, v, offsets)) and lse[:T].any(0).all()
+
+
+def test_offsets_of_another_number_of_prompts_are_refused(gen):
+    P, T, Hk, D = 2, 10, 2, 64
+    c, k = verify.PathCache(P, 1, 16, 1, Hk, Hk, D, 1), normal(gen, (T, Hk, D), BF)
+    zero = torch.zeros((P, 16, Hk, D), dtype=BF, device="cuda")
+    c.write_prompt(0, zero, zero)
+    for wrong in (ints([0, 4, 7, 10]), ints([0, 10]), ints([[0, 4, 10]]), ints([0, 4, 10, 10])):       # (a third prompt would be lost)
+        with pytest.raises(ValueError):
+            c.write_packed(0, k, k, wrong)
+    assert not c.read_prompt(0, 16)[0].any()
+    c.write_packed(0, k, k, ints([0, 4, 10]))
+    got = c.read_prompt(0, 16)[0]
+    assert same(got[0, :4], k[:4]) and same(got[1, :6], k[4:]) and not got[0, 4:].any() and not got[1, 6:].any()
