@@ -185,6 +185,7 @@ class PathCache:
         _check(load().csd_cache_bytes(ctypes.byref(self.cfg), ctypes.byref(nbytes)), "csd_cache_bytes")
         # +256 so that a 256-byte aligned start always exists inside the buffer
         self._buf = torch.empty(nbytes.value + 256, dtype=torch.uint8, device=self.device)
+        self._place = self._buf.get_device()
         self._ws = (self._buf.data_ptr() + 255) // 256 * 256
         _check(load().csd_cache_create(ctypes.byref(self.cfg), self._ws, nbytes.value, _stream(), ctypes.byref(self._h)),
                "csd_cache_create")
@@ -233,7 +234,10 @@ class PathCache:
     def write_rotated(self, layer, q, k, v, rotary, positions, start=None, counts=None):
         """What rotate() does to q [P][N][n][heads][head_dim] and k at positions [P][N][n] int32, and write() with the rotated keys and v, in
         one launch.  Returns the rotated queries, all n of each path."""
-        got = _native.cache_write_rotated(*self._cache(), torch._C._cuda_getDevice(), *rotary._call, layer, q, k, v, positions, start, counts)
+        here = torch._C._cuda_getDevice()
+        got = None
+        if here == self._place:
+            got = _native.cache_write_rotated(*self._cache(), here, *rotary._call, layer, q, k, v, positions, start, counts)
         if got is not None:
             _check(got[0], "csd_cache_write_rotated")
             return got[1]
@@ -242,7 +246,7 @@ class PathCache:
         qh = _heads(q, self.dtype, lead, c.n_heads, c.head_dim)
         kh, vh = (_heads(t, self.dtype, lead, c.n_kv_heads, c.head_dim) for t in (k, v))
         n = q.shape[-3]
-        _here(q, k, v, positions, start, counts)
+        _here(self._buf, q, k, v, positions, start, counts)
         if v.shape != k.shape or k.shape[-3] != n:
             raise ValueError("queries of shape %s, keys of %s, values of %s" % (tuple(q.shape), tuple(k.shape), tuple(v.shape)))
         if positions.shape != (*lead, n):
@@ -260,7 +264,7 @@ class PathCache:
         kh, vh = (_packed(t, self.dtype, c.n_kv_heads, c.head_dim) for t in (k, v))
         if v.shape != k.shape or k.dim() != 3:
             raise ValueError("keys of shape %s, values of shape %s" % (tuple(k.shape), tuple(v.shape)))
-        _here(offsets)
+        _here(self._buf, offsets)
         if offsets.shape != (self.P + 1,):
             raise ValueError("offsets of shape %s, needs %s" % (tuple(offsets.shape), (self.P + 1,)))
         _check(load().csd_cache_write_packed(self._h, layer, ctypes.byref(kh), ctypes.byref(vh), _ptr(offsets, torch.int32, self.P + 1),
