@@ -158,7 +158,7 @@ int csd_targets(const void* d_logits, int32_t type, int64_t rows, int32_t vocab,
                 void* stream);
 
 /* Rotary positions.  Pair i (of dim / 2) of a head at position t is turned by the angle 2 pi t turns[i]:
- *   (a, b) -> amplitude * (a cos - b sin, a sin + b cos), to 2^-35 of its terms, then rounded to 32 bits and to the type.
+ *   (a, b) -> amplitude * (a cos - b sin, a sin + b cos), to 3 * 2^-35 of its terms, then rounded to 32 bits and to the type.
  * Positions are whole numbers of any sign. */
 typedef struct {
   const double* d_turns; /* [dim / 2], device memory, 8-byte aligned: turns per token (csd_rotary_turns makes the usual ones)  */

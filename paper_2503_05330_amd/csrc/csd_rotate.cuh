@@ -3,8 +3,8 @@
 // Angles, sines and cosines are in 64 bits: a position (31 bits) times turns per token is off by 2^-22 turns at most, 2^-29 for a position of
 // 2^24, and whole turns are taken off it.  A workgroup's tokens have them in LDS, worked out once for all heads (64 pairs of eight tokens are one
 // evaluation a thread), each as a number of 12 bits and what is left of it, 24 bits.  A value has 8 or 11 bits, so its product with the first
-// is exact in 32 bits; the difference of two such products comes with its error, and the products of the rest are added to that: a
-// result is off by 2^-35 of its terms before it is rounded to 32 bits and to the type.  (Plain products in 32 bits put one of some 10^5 on
+// is exact in 32 bits; the difference of two such products comes with its error, and the products of the rest are added to that, three
+// roundings of numbers below 2^-11 of the terms: a result is off by 3 * 2^-35 of its terms before it is rounded to 32 bits and to the type.  (Plain products in 32 bits put one of some 10^5 on
 // the other side of a rounding to 16 bits, and a code of 8 bits with it, at no less time: 72 us for 70 with 64 x 16 x 9 tokens of
 // 32 + 8 heads of 128 to 8 bits, their reading included.)
 #pragma once
