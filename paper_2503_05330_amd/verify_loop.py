@@ -71,7 +71,7 @@ class Loop:
     """P x N paths that continue P prompts by up to path_cap tokens each.
 
     prompts: a tensor [P][T], or a list of tensors of different lengths.  penalties [P][3] (repetition, presence, frequency) and bias
-    [P][vocab] or [vocab], float32: see verify.adjust; the prompt's last token is the first that a path has said."""
+    [P][vocab] or [vocab], float32: see verify.adjust; a path has said what was sampled for it, and the drafted tokens before a position."""
 
     def __init__(self, model, prompts, paths, path_cap, query_len=3, draft_len=8, inv_temperature=1.0, greedy=False, fp8=False, seed=1,
                  penalties=None, bias=None):
@@ -97,7 +97,7 @@ class Loop:
         self.draft = None
         self.accepted = torch.zeros((), dtype=torch.int64, device=dev)
         self.penalties, self.bias = penalties, bias
-        if penalties is not None:                        # what the paths have said, and their prompts
+        if penalties is not None:                        # the paths' tokens, behind their prompts' last, and the prompts
             self.said = torch.zeros((P, paths, path_cap + draft_len + 1), dtype=torch.int32, device=dev)
             self.asked = torch.nn.utils.rnn.pad_sequence([x for x in prompts], batch_first=True).to(torch.int32)
             self.asked_len = torch.tensor([len(x) for x in prompts], dtype=torch.int32).to(dev)
@@ -147,7 +147,7 @@ class Loop:
             return logits if self.bias is None else verify.adjust(logits, counts=counts, bias=self.bias, out=logits)
         at = self.length.long()[..., None] + torch.arange(n, device=tokens.device)
         self.said.scatter_(-1, at.clamp(max=self.said.shape[-1] - 1), tokens)
-        return verify.adjust(logits, self.said, self.length + counts, counts, self.asked, self.asked_len, self.penalties, self.bias, out=logits)
+        return verify.adjust(logits, self.said[..., 1:], self.length + counts - 1, counts, self.asked, self.asked_len, self.penalties, self.bias, out=logits)
 
     def step(self):
         """One verifying pass: returns the model's tokens [P][N][n] and how many of them each path takes [P][N]."""
