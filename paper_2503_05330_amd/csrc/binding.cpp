@@ -495,7 +495,7 @@ struct Rotation {
 };
 
 // Tokens [..., heads, D] of `type`, the leading axes evenly spaced; *n is set where it is below 0, and has to be the tensor's tokens where not.
-csd_heads packed_of(Call& c, const Device& d, at::ScalarType type, int64_t heads, int64_t D, int64_t* n, const at::Tensor** of = nullptr) {
+csd_heads packed_of(Call& c, const Device& d, at::ScalarType type, int64_t heads, int64_t D, int64_t* n) {
   const at::Tensor* t = c.any_tensor();
   if (!t || t->dim() < 3 || t->scalar_type() != type) {
     c.usual = false;
@@ -510,10 +510,9 @@ csd_heads packed_of(Call& c, const Device& d, at::ScalarType type, int64_t heads
   if (tokens != *n || tokens == 0 || sizes[axes] != heads || sizes[axes + 1] != D || strides[axes + 1] != 1) c.usual = false;
   const csd_heads h{t->data_ptr(), 0, spacing(c, sizes, strides, axes), heads > 1 ? strides[axes] : 0};
   if (reinterpret_cast<uintptr_t>(h.data) % 16 || h.token_stride % 8 || h.head_stride % 8) c.usual = false;
-  if (of) *of = t;
   return h;
 }
-// contiguous, of exactly these many numbers
+// contiguous, of these many numbers at least
 const int32_t* ints_of(Call& c, const Device& d, int64_t numel, bool maybe) {
   const at::Tensor* t = c.any_tensor(maybe);
   if (!t) return nullptr;

@@ -87,11 +87,11 @@ __device__ inline const uint8_t* uniform(const uint8_t* p) {
 __device__ inline void fetch(uint32_t lds, const uint8_t* from, const uint32_t (&source)[4]) {
   asm volatile(
       "s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
-      "global_load_lds_dwordx4 %2, %5 offset:1024\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048\n\t"
+      "global_load_lds_dwordx4 %2, %5 offset:0x400\n\tglobal_load_lds_dwordx4 %3, %5 offset:0x800\n\t"
       "global_load_lds_dwordx4 %4, %5 offset:0xc00" ::"s"(lds), "v"(source[0]), "v"(source[1]), "v"(source[2]), "v"(source[3]), "s"(from) : "m0", "memory");
 }
 __device__ inline void fetch(uint32_t lds, const uint8_t* from, const uint32_t (&source)[2]) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds),
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:0x400" ::"s"(lds),
                "v"(source[0]), "v"(source[1]), "s"(from) : "m0", "memory");
 }
 __device__ inline void fetch(uint32_t lds, const uint8_t* from, uint32_t source) {

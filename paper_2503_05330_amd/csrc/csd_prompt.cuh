@@ -40,9 +40,9 @@ constexpr int kPromptTile = 2 * kBlock, kPromptStages = 2;
 // its place, of the sequence's last token (`left`: its tokens from the tile's first on) where there is none.
 template <class R, int WAVES>
 struct TileLoads {
-  static constexpr int kAll = 2 * R::kPieces, kPieces = (kAll + WAVES - 1) / WAVES;              // piece wave + WAVES x, where it is one of all
+  static_assert(2 * R::kPieces % WAVES == 0, "");
+  static constexpr int kPieces = 2 * R::kPieces / WAVES;                                         // wave + WAVES x
   static constexpr int kApart = 64 * WAVES / R::kChunks;                                         // tokens from one to the next, where chunks are a power of two
-  static __device__ bool there(int x, int wave) { return kAll % WAVES == 0 || wave + WAVES * x < kAll; }
   // The lane's places in pieces x and x + kOrders lie whole tokens apart, which a wave's address takes: their chunks are in the same order.  (The order is
   // part of the place: a turn put on a sum of tokens and chunks also meets bits of the tokens' where strides are no multiples of 32.)
   static constexpr int orders() {
@@ -71,13 +71,13 @@ struct TileLoads {
   __device__ void fetch_to(uint32_t lds, const One* from, int64_t stride, int wave) const {
 #pragma unroll
     for (int x = 0; x < kPieces; ++x)
-      if (there(x, wave)) fetch(uniform(lds + 1024u * (WAVES * x + wave)), uniform(reinterpret_cast<const uint8_t*>(from + wave_at(x, stride))), lane_at(x));
+      fetch(uniform(lds + 1024u * (WAVES * x + wave)), uniform(reinterpret_cast<const uint8_t*>(from + wave_at(x, stride))), lane_at(x));
   }
   template <class One>
   static __device__ void fetch_part(uint32_t lds, const One* from, int64_t stride, int32_t left, int wave, int lane) {
 #pragma unroll
     for (int x = 0; x < kPieces; ++x)
-      if (there(x, wave)) fetch(uniform(lds + 1024u * (WAVES * x + wave)), uniform(reinterpret_cast<const uint8_t*>(from)), place(x, stride, left, wave, lane));
+      fetch(uniform(lds + 1024u * (WAVES * x + wave)), uniform(reinterpret_cast<const uint8_t*>(from)), place(x, stride, left, wave, lane));
   }
 };
 
