@@ -6,14 +6,20 @@
 // with a running (near) maximum and sum, no weight leaving its lane.  Keys and values come in tiles of 64 tokens to a ring of two in
 // LDS, by loads that pass no register, the next tile's during the products of one; all waves of the workgroup read the same (or,
 // where two share a row, a block each).
+// Scores, maxima, sums and O are in 32 bits.  A weight is rounded to the tensors' type, to nearest, for the second product, as in csd_attend.cuh: the
+// matrix cores take no other operand at that rate (as two numbers of 16 bits it would cost half as many products again).  That is off by
+// 2^-8 (half precision: 2^-11) of the weight at most, to either side.  Against 64 bits results of 16384 tokens are off by 0.0020 in the mean
+// (half precision, 5 of 331 .. 777: 0.00025); with weights in 32 bits, by the results' own rounding, 0.0015 (0.0002).
 // Tiles that all rows see whole come first, without a mask; the last few, of which rows see a part, are edge()'s.
 //
 // What bounds it: at length power, then LDS.  One sequence of 16384 tokens, 28 heads of 128 on 4: 1.66 .. 1.74 ms, 1100 .. 1160 TFLOP/s (a product
-// of 16384^3 reaches 1360; this kernel 1460 with operands of zeros, at which the clock stays up).  8 x 4096, 32 on 8: 1.05 ms, 1050.  A wave's operands from
+// of 16384^3 reaches 1360; this kernel 1460 with operands of zeros, at which the clock stays up).  8 x 4096, 32 on 8: 1.05 .. 1.07 ms, 1040.  A wave's operands from
 // LDS, 32 rows a wave, take about as long as the products.  64 rows a wave, half of these reads, leave one wave a SIMD: its accumulators move
-// between register files, 1.78 us a tile of 256 rows for 1.5, and 25 us before and behind.  Short ones are bound by what comes one after the
-// other: 0.75 .. 0.95 us a tile of 64 tokens for a wave, 6.5 us of launch, first loads and results.  5 sequences of 331 .. 777 tokens, 12 heads of 64:
-// 12.2 us; 16 of 1 .. 1024, 32 on 8 of 128: 75 .. 82 (35 at the rate of a large product).
+// between register files, 1.78 us a tile of 256 rows for 1.5, and 25 us before and behind.  Heads of 64 have the softmax of as many scores beside half the products: 4 x 8192, 16 heads, 620 .. 685 us, matrix cores busy 52 % of
+// the CUs' cycles.  Heads of 96 have conflicts in 60 % of LDS's cycles: 8192, 32 on 8, 470 .. 500, 42 %.  Heads of 256 have one wave a SIMD: 8192, 16 on
+// 8, 620 .. 680, 37 %.  Short ones are bound by what comes one after the other: 0.75 .. 0.95 us a tile of 64 tokens for a wave, 6.5 us of launch, first
+// loads and results.  5 sequences of 331 .. 777 tokens, 12 heads of 64: 12.1 us among others, 14 .. 16 by itself; 16 of 1 .. 1024, 32 on 8 of 128: 75 .. 82 (35 at
+// the rate of a copy).
 //
 // Scores of the next tile before the softmax of one, which would keep the matrix cores busy with one wave, spill; with two waves a SIMD the other
 // does that.  Four tiles in LDS instead of two leave one workgroup a CU, and gained nothing.

@@ -4,9 +4,9 @@
 // 2^24, and whole turns are taken off it.  A workgroup's tokens have them in LDS, worked out once for all heads (64 pairs of eight tokens are one
 // evaluation a thread), each as a number of 12 bits and what is left of it, 24 bits.  A value has 8 or 11 bits, so its product with the first
 // is exact in 32 bits; the difference of two such products comes with its error, and the products of the rest are added to that, three
-// roundings of numbers below 2^-11 of the terms: a result is off by 3 * 2^-35 of its terms before it is rounded to 32 bits and to the type.  (Plain products in 32 bits put one of some 10^5 on
-// the other side of a rounding to 16 bits, and a code of 8 bits with it, at no less time: 72 us for 70 with 64 x 16 x 9 tokens of
-// 32 + 8 heads of 128 to 8 bits, their reading included.)
+// roundings of numbers below 2^-11 of the terms: a result is off by 3 * 2^-35 of its terms before it is rounded to 32 bits and to the
+// type.  (Plain products in 32 bits put one of some 10^5 on the other side of a rounding to 16 bits, and a code of 8 bits with it, at no less
+// time: 72 us for 70 with 64 x 16 x 9 tokens of 32 + 8 heads of 128 to 8 bits, their reading included.)
 #pragma once
 
 #include "csd_verify.cuh"
@@ -34,7 +34,7 @@ __device__ inline Turn turn_of(const csd_rotary& how, int32_t position, int pair
 }
 
 // A token's pairs in LDS.  Lanes that read together take the same of eight neighbours, so these lie side by side; a token's pairs are 16 bytes more
-// than its eights fill, which puts the tokens on different banks.  (In plain order 8 x 4096 tokens of 40 heads of 128 took 285 us for 131.)
+// than its eights fill, which puts most tokens on different banks.  (In plain order 8 x 4096 tokens of 40 heads of 128 took 285 us for 131.)
 struct Turns {
   Turn* of;
   int32_t eights;                                          // of pairs

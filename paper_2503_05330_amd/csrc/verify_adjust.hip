@@ -8,8 +8,10 @@
 // logits are copied, with their bias and bit of the mask.  Every workgroup of a path reads all of the prompt's and the path's tokens, from L2; the
 // logits' first vectors are asked for before the counting.
 //
-// What bounds it: memory.  64 paths x up to 17 positions of 152064 in bfloat16, a prompt of 4096 tokens, paths of up to 4096, masks: 117 us, 4.4
-// TB/s (a copy reaches 5.2); 3 x 13 x 5 of 50257 in 32 bits, biases: 15.4 us, 4.1 TB/s; 4 x 32000: 5.8 us, a launch and three round trips.
+// What bounds it: memory, and the counting where positions are few.  64 paths x up to 17 positions of 152064 in bfloat16, a prompt of 4096 tokens, paths
+// of up to 4096, masks: 110 .. 119 us, 4.4 TB/s (a copy reaches 5.2); with all positions there 155, 133 without penalties.  1024 paths x 1 position
+// 180; 166 without masks, 115 without penalties.  (Every lane reads the words of its eight logits at once: 70 .. 85 % of LDS's cycles are conflicts.)  3 x 13 x 5 of 50257
+// in 32 bits, biases: 15.6 us, 4.1 TB/s; 4 x 32000: 5.5 us, a launch and three round trips.
 #include "csd_verify.cuh"
 
 namespace csd {
@@ -205,8 +207,8 @@ extern "C" int csd_adjust(const csd_adjustment* adjustment, void* stream) {
   if (a.d_prompt && (a.prompt_stride < 0 || a.prompt_cap < 0 || a.prompt_cap > CSD_MAX_CACHE_TOKENS)) return CSD_ERR_INVALID_ARG;
   if ((a.d_bias && a.bias_stride < 0) || (a.d_mask && a.mask_stride < 0)) return CSD_ERR_INVALID_ARG;
   // Stretches: as long as leaves some 1024 workgroups, up to a bound.  Short ones read and count the tokens more often, which weighs with few positions;
-  // long ones have more in LDS, and fewer workgroups a CU.  us with 2048, 4096 and 8192 logits, vocabulary 152064, 4096 + 4096 tokens: 1024
-  // paths x 1 position 373, 261, 180; 256 x 4 141, 116, 114; 128 x 8 107, 110, 119; 64 x 17 117, 130, 146.
+  // long ones have more in LDS, and fewer workgroups a CU.  us with 2048, 4096 and 8192 logits, vocabulary 152064, 4096 + 4096 tokens, masks:
+  // 1024 paths x 1 position 373, 261, 180; 256 x 4 141, 116, 114; 128 x 8 107, 110, 119; 64 x 17 117, 130, 146.
   const int32_t longest = a.n <= 4 ? 8192 : a.n < 8 ? 4096 : 2048;
   int64_t parts = (1024 + paths - 1) / paths;
   const int64_t most = (a.vocab + kLeastStretch - 1) / kLeastStretch, least = (a.vocab + longest - 1) / longest;

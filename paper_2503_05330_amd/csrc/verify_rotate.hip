@@ -2,10 +2,10 @@
 //
 // A workgroup has eight tokens: their pairs' turns are worked out once, in LDS, and serve all heads.  What bounds it: memory.  8 x 4096 tokens of 40
 // heads of 128: 131 us, 5.1 TB/s, what a copy reaches; sixteen tokens 4.3 us, launch and round trips.  With the write, 64 x 16 x 9
-// tokens of 32 + 8 + 8 heads, to 8 bits: 42 us of 66 with their reading, 4.3 TB/s.  One launch instead of two saves keys a write and a read, and
+// tokens of 32 + 8 + 8 heads, to 8 bits: 47 us of 66 with their reading, 3.85 TB/s.  One launch instead of two saves keys a write and a read, and
 // the launch.  Of queries a thread holds both eights of eight pairs (as keys are, an eight at a time with its pairs' others read beside: 69.5; queries
-// before keys: 67.4).  (Asking for the next values before one is turned: 3 us more; six waves a SIMD, by spilling: 30 more; banks'
-// conflicts of the turns' reads taken away, sines of a shorter series, workgroups of half the heads: the same.)
+// before keys: 67.4).  (Asking for the next values before one is turned: 3 us more; six waves a SIMD, by spilling: 30 more; the banks'
+// conflicts that the turns' reads have, 15 .. 44 % of LDS's cycles, taken away, sines of a shorter series, workgroups of half the heads: the same.)
 #include <cmath>
 
 #include "csd_cache.cuh"
